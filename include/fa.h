@@ -325,6 +325,95 @@ fa_status fa_poll_status(const fa_cache* cache, void* stream);
  * form is the same kernels, plus the append kernel with more than four query heads to a KV head).  Unknown values of what return 0. */
 int fa_launch_count(const fa_layout* layout, int what);
 
+/* ---- Dense cache in 8 bits ------------------------------------------------------------------------------------------
+ * For layers whose K and V are kept whole (no dimension compressed): the tokens of a row in blocks of `block`
+ * tokens.  A complete block of one KV head is a page of 8-bit values, token-major, with one scale for K and one for V;
+ * the block under construction is the row's tail, kept in kv_dtype.  So every value is rounded once, when its
+ * block is complete, and the cache is a function of the tokens alone, not of the calls that brought them.
+ *   FA_Q8_INT8  scale = amax / 127, value = x * 127 / amax rounded to a whole number (half to even)
+ *   FA_Q8_E4M3  scale = amax / 448, value = x * 448 / amax rounded to e4m3 (half to even)
+ * with amax the largest magnitude of the block's values of that head and side; the value is that of the exact quotient, the scale is
+ * rounded to 32 bits (down where top * scale would overflow).  A block of zeros has scale 0; a block with a value that is not finite has scale NaN and reads
+ * as NaN throughout (attention treats a tail that holds one the same way).
+ * Pages are found by a block table, so rows may share pages that they only read (a common prompt), and pages need no order.
+ * A block needs its page when it becomes complete; entries of later blocks are not read. */
+typedef enum { FA_Q8_INT8 = 0, FA_Q8_E4M3 = 1 } fa_q8_format;
+
+typedef struct fa_q8_layout {
+    int32_t batch;          /* B, at most 65535                                         */
+    int32_t n_q_heads;      /* H_q; query head g reads KV head g / (H_q / H_kv), at most 16 to a KV head */
+    int32_t n_kv_heads;     /* H_kv, divides H_q                                        */
+    int32_t head_dim;       /* d: 64, 128 or 256                                        */
+    int32_t block;          /* tokens of a block: 16, 32, 64 or 128                     */
+    int32_t max_blocks;     /* entries of a row of the block table; a row holds at most max_blocks * block tokens */
+    int32_t n_pages;        /* pages of k_pages / v_pages                               */
+    int32_t format;         /* fa_q8_format                                             */
+    int32_t kv_dtype;       /* fa_dtype of K, V, q, out and of the tails                */
+    float   softmax_scale;  /* logits = softmax_scale * q . k                           */
+} fa_q8_layout;
+
+typedef struct fa_q8_cache {
+    uint8_t* k_pages;             /* [n_pages][H_kv][block][d]                                */
+    uint8_t* v_pages;
+    float*   k_scale;             /* [n_pages][H_kv]                                          */
+    float*   v_scale;
+    void*    k_tail;              /* [B][H_kv][block][d]; rows behind the row's last token are left as they were */
+    void*    v_tail;
+    float*   tail_amax;           /* [B][H_kv][2] largest magnitude of the tail's K and V (written by the calls) */
+    const int32_t* block_table;   /* [B][max_blocks] page of every block                      */
+    int32_t* state;               /* [B][4]: tokens of the row, scratch (zero between calls), 2 spare */
+    int32_t* status;              /* [4]: sticky fa_status word, ticket (zero between calls), 2 spare */
+} fa_q8_cache;
+
+typedef struct fa_q8_cache_sizes {
+    size_t k_pages, v_pages, k_scale, v_scale, k_tail, v_tail, tail_amax, block_table, state, status;
+} fa_q8_cache_sizes;
+
+/* Host only.  Checks the layout and fills *out. */
+fa_status fa_q8_cache_sizes_of(const fa_q8_layout* layout, fa_q8_cache_sizes* out);
+
+/* Host only.  Bytes of workspace fa_q8_attention needs for up to n_q queries a row (fa_q8_step: 1).  The rule of
+ * fa_workspace_bytes holds: zero the first 4 KiB once (fa_workspace_init), every call leaves them at zero.  Calls
+ * that may overlap on the GPU need workspaces of their own. */
+fa_status fa_q8_workspace_bytes(const fa_q8_layout* layout, int32_t n_q, size_t* out);
+
+/* Empties all rows and clears the status (pages and tails keep their bytes). */
+fa_status fa_q8_reset(const fa_q8_layout* layout, fa_q8_cache* cache, void* stream);
+
+/* K, V: tokens, element (b, t, h, e) at b*stride_b + t*stride_t + h*stride_h + e (strides in elements, multiples of 8, as for
+ * fa_compress), n tokens a row; n_row: optional DEVICE array [B], row b brings its first n_row[b] tokens only
+ * (0 <= n_row[b] <= n; others are clamped).  fa_q8_write makes a row consist of these tokens, fa_q8_append puts them behind its own.
+ * A row that would exceed max_blocks * block tokens keeps its tokens and FA_ERR_CAPACITY is reported.  A row that needs
+ * a page outside 0..n_pages-1 for a block that the call completes: FA_ERR_INDEX, fa_q8_append leaves it its tokens, fa_q8_write leaves it empty (in
+ * both cases the good pages of the other blocks may have been written).  Two rows must not complete blocks in one page. */
+fa_status fa_q8_write(const fa_q8_layout* layout, fa_q8_cache* cache, const void* K, const void* V, int64_t stride_b,
+                      int64_t stride_t, int64_t stride_h, int32_t n, const int32_t* n_row, void* stream);
+fa_status fa_q8_append(const fa_q8_layout* layout, fa_q8_cache* cache, const void* K, const void* V, int64_t stride_b,
+                       int64_t stride_t, int64_t stride_h, int32_t n, const int32_t* n_row, void* stream);
+
+/* Reads tokens t0 .. t0 + n - 1 of every row back into K, V (strides as above) in kv_dtype: value * scale for pages,
+ * the tail's rows as they are.  Ready for fa_compress or fa_select_dims.  What a row does not hold leaves K and V
+ * as they were (so do tokens whose page is out of range: FA_ERR_INDEX). */
+fa_status fa_q8_read(const fa_q8_layout* layout, const fa_q8_cache* cache, void* K, void* V, int64_t stride_b,
+                     int64_t stride_t, int64_t stride_h, int32_t t0, int32_t n, void* stream);
+
+/* Softmax attention of n_q queries a row over the cached tokens.  q: element (b, i, g, e) at b*stride_b + i*stride_i +
+ * g*stride_g + e (strides in elements, multiples of 8); out: [B][n_q][H_q][d].  The queries are those of the row's
+ * last n_q tokens, whose K and V the cache holds already: query i sees tokens 0 .. len - n_q + i.  A query that sees none (an empty
+ * row, or a row of fewer than n_q tokens) gives zeros.  Does not modify the cache.  Tokens whose page is out of range are
+ * left out and FA_ERR_INDEX is reported. */
+fa_status fa_q8_attention(const fa_q8_layout* layout, const fa_q8_cache* cache, const void* q, int64_t stride_b, int64_t stride_i,
+                          int64_t stride_g, void* out, int32_t n_q, void* ws, size_t ws_bytes, void* stream);
+
+/* One decode step: the result and the cache afterwards are those of fa_q8_append(k_new, v_new) with one token a row
+ * and fa_q8_attention(q) with one query, as one launch.  q, out [B][H_q][d], k_new, v_new [B][H_kv][d].  A row whose push is refused (FA_ERR_CAPACITY,
+ * FA_ERR_INDEX) attends to its unchanged tokens. */
+fa_status fa_q8_step(const fa_q8_layout* layout, fa_q8_cache* cache, const void* q, const void* k_new, const void* v_new,
+                     void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* fa_poll_status of a cache in 8 bits. */
+fa_status fa_q8_poll_status(const fa_q8_cache* cache, void* stream);
+
 const char* fa_status_string(fa_status s);
 int fa_version(void);
 

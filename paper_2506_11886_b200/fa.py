@@ -22,6 +22,7 @@ FA_F32, FA_BF16 = 0, 1
 FA_NORM_ORTHO, FA_NORM_PAPER = 0, 1
 FA_DECODE_AUTO, FA_DECODE_DIRECT, FA_DECODE_FFT, FA_DECODE_FFT_SPLIT = 0, 1, 2, 3
 FA_COMPRESS_ORDERED, FA_COMPRESS_FFT = 1, 2
+FA_Q8_INT8, FA_Q8_E4M3 = 0, 1
 
 
 class fa_layout(C.Structure):
@@ -40,6 +41,22 @@ class fa_cache(C.Structure):
 
 class fa_cache_sizes(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in _CACHE_FIELDS]
+
+
+class fa_q8_layout(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "block", "max_blocks", "n_pages", "format",
+                                         "kv_dtype")] + [("softmax_scale", C.c_float)]
+
+
+_Q8_FIELDS = ("k_pages", "v_pages", "k_scale", "v_scale", "k_tail", "v_tail", "tail_amax", "block_table", "state", "status")
+
+
+class fa_q8_cache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in _Q8_FIELDS]
+
+
+class fa_q8_cache_sizes(C.Structure):
+    _fields_ = [(n, C.c_size_t) for n in _Q8_FIELDS]
 
 
 class FaError(RuntimeError):
@@ -85,11 +102,22 @@ def lib() -> C.CDLL:
         L.fa_step_staging_bytes.argtypes = [lp]
         L.fa_step_staging_bytes.restype = sz
         L.fa_launch_count.argtypes = [lp, C.c_int]
+        qp, qc = C.POINTER(fa_q8_layout), C.POINTER(fa_q8_cache)
+        L.fa_q8_cache_sizes_of.argtypes = [qp, C.POINTER(fa_q8_cache_sizes)]
+        L.fa_q8_workspace_bytes.argtypes = [qp, i32, C.POINTER(sz)]
+        L.fa_q8_reset.argtypes = [qp, qc, vp]
+        L.fa_q8_write.argtypes = L.fa_q8_append.argtypes = [qp, qc, vp, vp, i64, i64, i64, i32, vp, vp]
+        L.fa_q8_read.argtypes = [qp, qc, vp, vp, i64, i64, i64, i32, i32, vp]
+        L.fa_q8_attention.argtypes = [qp, qc, vp, i64, i64, i64, vp, i32, vp, sz, vp]
+        L.fa_q8_step.argtypes = [qp, qc, vp, vp, vp, vp, vp, sz, vp]
+        L.fa_q8_poll_status.argtypes = [qc, vp]
         L.fa_status_string.argtypes = [C.c_int]
         L.fa_status_string.restype = C.c_char_p
         for name in ("fa_cache_sizes_of", "fa_workspace_bytes", "fa_cache_reset", "fa_validate", "fa_compress",
                      "fa_append", "fa_decode_attention", "fa_poll_status", "fa_launch_count", "fa_version",
-                     "fa_decode_step_host", "fa_decode_step", "fa_select_workspace_bytes", "fa_select_dims", "fa_compress_ragged", "fa_workspace_init"):
+                     "fa_decode_step_host", "fa_decode_step", "fa_select_workspace_bytes", "fa_select_dims", "fa_compress_ragged", "fa_workspace_init",
+                     "fa_q8_cache_sizes_of", "fa_q8_workspace_bytes", "fa_q8_reset", "fa_q8_write", "fa_q8_append", "fa_q8_read", "fa_q8_attention",
+                     "fa_q8_step", "fa_q8_poll_status"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -413,3 +441,183 @@ def fa_decode_attention_static(layout: Layout, cache: Cache, q: torch.Tensor, ou
     f.restype = C.c_int
     f.argtypes = [C.POINTER(fa_layout), C.POINTER(fa_cache), C.c_void_p, C.c_void_p, C.c_void_p]
     _check(f(layout.ref(), cache.ref(), _ptr(q), _ptr(out), _stream(stream)), "fa_decode_attention_static")
+
+
+# ---- dense cache in 8 bits ----------------------------------------------------------------------------------------
+@dataclass
+class Q8Layout:
+    """Python mirror of ``fa_q8_layout`` (field meanings: include/fa.h)."""
+    batch: int
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+    block: int
+    max_blocks: int
+    n_pages: int
+    format: int = FA_Q8_INT8
+    kv_dtype: int = FA_BF16
+    softmax_scale: float = 1.0
+
+    def __setattr__(self, name, value):
+        self.__dict__.pop("_cref", None)
+        self.__dict__[name] = value
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_cref"}
+
+    def ref(self):
+        r = self.__dict__.get("_cref")
+        if r is None:
+            r = self.__dict__["_cref"] = C.byref(self.c())
+        return r
+
+    def c(self) -> fa_q8_layout:
+        return fa_q8_layout(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.block, self.max_blocks, self.n_pages,
+                            self.format, self.kv_dtype, float(self.softmax_scale))
+
+    @property
+    def torch_dtype(self) -> torch.dtype:
+        return torch.bfloat16 if self.kv_dtype == FA_BF16 else torch.float32
+
+    @property
+    def page_dtype(self) -> torch.dtype:
+        return torch.int8 if self.format == FA_Q8_INT8 else torch.float8_e4m3fn
+
+
+def fa_q8_cache_sizes_of(layout: Q8Layout) -> dict:
+    out = fa_q8_cache_sizes()
+    _check(lib().fa_q8_cache_sizes_of(layout.ref(), C.byref(out)), "fa_q8_cache_sizes_of")
+    return {n: int(getattr(out, n)) for n in _Q8_FIELDS}
+
+
+def fa_q8_workspace_bytes(layout: Q8Layout, n_q: int = 1) -> int:
+    out = C.c_size_t(0)
+    _check(lib().fa_q8_workspace_bytes(layout.ref(), int(n_q), C.byref(out)), "fa_q8_workspace_bytes")
+    return int(out.value)
+
+
+class Q8Cache:
+    """Device buffers of one layer's dense cache in 8 bits: ``k_pages`` [n_pages][H_kv][block][d] in the format's dtype,
+    ``k_scale`` [n_pages][H_kv], ``k_tail`` [B][H_kv][block][d], ``block_table`` [B][max_blocks] int32, ``state`` [B][4] (column 0: tokens of the
+    row), ...  ``buffers``: tensors to be used instead of new ones, by name (contiguous, of these shapes; an
+    engine's own pages, say).  A new block table gives page b * max_blocks + i to block i of row b, as far as there are pages (-1 past them)."""
+
+    def __init__(self, layout: Q8Layout, buffers=None, device="cuda"):
+        self.layout = layout
+        given = dict(buffers or {})
+        L, dt = layout, layout.torch_dtype
+        sizes = fa_q8_cache_sizes_of(layout)
+        B, H, blk, d = L.batch, L.n_kv_heads, L.block, L.head_dim
+        shapes = dict(k_pages=((L.n_pages, H, blk, d), L.page_dtype), k_scale=((L.n_pages, H), torch.float32), k_tail=((B, H, blk, d), dt),
+                      tail_amax=((B, H, 2), torch.float32), block_table=((B, L.max_blocks), torch.int32), state=((B, 4), torch.int32),
+                      status=((4,), torch.int32))
+        shapes.update({"v" + n[1:]: shapes[n] for n in ("k_pages", "k_scale", "k_tail")})
+        unknown = set(given) - set(_Q8_FIELDS)
+        if unknown:
+            raise ValueError(f"Q8Cache: no buffer is called {sorted(unknown)}")
+        dev = next((t.device for t in given.values()), torch.device(device))
+        for n in _Q8_FIELDS:
+            shape, dtype = shapes[n]
+            t = given.get(n)
+            if t is None:
+                t = torch.zeros(shape, dtype=torch.uint8 if dtype == torch.float8_e4m3fn else dtype, device=dev)
+                t = t.view(dtype)
+                if n == "block_table":
+                    own = torch.arange(B * L.max_blocks, dtype=torch.int32, device=dev).reshape(shape)
+                    t.copy_(torch.where(own < L.n_pages, own, -1))
+            elif tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or t.device != dev:
+                raise ValueError(f"Q8Cache: {n} has to be contiguous {shape} {dtype} on {dev}")
+            assert t.numel() * t.element_size() == sizes[n], (n, t.shape, sizes[n])
+            setattr(self, n, t)
+        self.device = dev
+        self._c = fa_q8_cache(*[_ptr(getattr(self, n)) for n in _Q8_FIELDS])
+        self._cref = C.byref(self._c)
+
+    def c(self) -> fa_q8_cache:
+        return self._c
+
+    def ref(self):
+        return self._cref
+
+
+def new_q8_workspace(layout: Q8Layout, n_q: int = 1, device="cuda") -> torch.Tensor:
+    """A zero-filled workspace of fa_q8_attention for up to n_q queries a row, and of fa_q8_step."""
+    return torch.zeros(fa_q8_workspace_bytes(layout, n_q), dtype=torch.uint8, device=device)
+
+
+def fa_q8_reset(layout: Q8Layout, cache: Q8Cache, stream=None) -> None:
+    _check(lib().fa_q8_reset(layout.ref(), cache._cref, _stream(stream)), "fa_q8_reset")
+
+
+def _q8_tokens(layout: Q8Layout, K: torch.Tensor, V: torch.Tensor, what: str):
+    """Strides and count of [B][n][H_kv][d] tensors."""
+    shape = K.shape
+    if (len(shape) != 4 or shape[0] != layout.batch or shape[2] != layout.n_kv_heads or shape[3] != layout.head_dim or V.shape != shape
+            or K.dtype != layout.torch_dtype or V.dtype != K.dtype or not K.is_cuda or not V.is_cuda):
+        raise ValueError(f"{what}: K and V have to be [B][n][H_kv][d] tensors of the layout on the GPU")
+    st = K.stride()
+    if st != V.stride() or (shape[1] and st[3] != 1):
+        raise ValueError(f"{what}: K and V have to have the same strides, 1 along d")
+    # strides of axes that have one entry are never used
+    d = shape[3]
+    return (st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else d, st[2] if shape[2] > 1 else d, shape[1])
+
+
+def _q8_store(call, what, layout, cache, K, V, n_row, stream):
+    sb, st, sh, n = _q8_tokens(layout, K, V, what)
+    if n_row is not None and (n_row.dtype != torch.int32 or n_row.shape != (layout.batch,) or not n_row.is_cuda or not n_row.is_contiguous()):
+        raise ValueError(f"{what}: n_row has to be an int32 tensor [B] on the GPU")
+    status = call(layout.ref(), cache._cref, K.data_ptr(), V.data_ptr(), sb, st, sh, n, 0 if n_row is None else n_row.data_ptr(), _stream(stream))
+    if status:
+        _check(status, what)
+
+
+def fa_q8_write(layout: Q8Layout, cache: Q8Cache, K: torch.Tensor, V: torch.Tensor, n_row=None, stream=None) -> None:
+    """Every row becomes the tokens K, V [B][n][H_kv][d] (any strides with unit stride on d), row b their first n_row[b] only."""
+    _q8_store(lib().fa_q8_write, "fa_q8_write", layout, cache, K, V, n_row, stream)
+
+
+def fa_q8_append(layout: Q8Layout, cache: Q8Cache, K: torch.Tensor, V: torch.Tensor, n_row=None, stream=None) -> None:
+    """The tokens K, V [B][n][H_kv][d] are put behind those of the rows."""
+    _q8_store(lib().fa_q8_append, "fa_q8_append", layout, cache, K, V, n_row, stream)
+
+
+def fa_q8_read(layout: Q8Layout, cache: Q8Cache, K: torch.Tensor, V: torch.Tensor, t0: int = 0, stream=None) -> None:
+    """Tokens t0 .. t0 + n - 1 into K, V [B][n][H_kv][d]; what a row does not hold stays as it is there."""
+    sb, st, sh, n = _q8_tokens(layout, K, V, "fa_q8_read")
+    status = lib().fa_q8_read(layout.ref(), cache._cref, K.data_ptr(), V.data_ptr(), sb, st, sh, t0, n, _stream(stream))
+    if status:
+        _check(status, "fa_q8_read")
+
+
+def fa_q8_attention(layout: Q8Layout, cache: Q8Cache, q: torch.Tensor, out: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """q [B][n_q][H_q][d] (any strides with unit stride on d), out contiguous [B][n_q][H_q][d]; or [B][H_q][d] both, for one query a row."""
+    shape, st = q.shape, q.stride()
+    if len(shape) == 3:
+        n_q, si = 1, layout.head_dim
+    else:
+        n_q, si = shape[1], (st[1] if shape[1] > 1 else layout.head_dim)
+    if (shape[0] != layout.batch or shape[-2] != layout.n_q_heads or shape[-1] != layout.head_dim or len(shape) not in (3, 4) or out.shape != shape
+            or q.dtype != layout.torch_dtype or out.dtype != q.dtype or not q.is_cuda or not out.is_cuda or not out.is_contiguous() or st[-1] != 1):
+        raise ValueError("fa_q8_attention: q and out have to be [B][n_q][H_q][d] or [B][H_q][d] tensors of the layout on the GPU, out contiguous")
+    status = lib().fa_q8_attention(layout.ref(), cache._cref, q.data_ptr(), st[0] if shape[0] > 1 else 0, si, st[-2] if shape[-2] > 1 else layout.head_dim,
+                                   out.data_ptr(), n_q, ws.data_ptr(), ws.numel(), _stream(stream))
+    if status:
+        _check(status, "fa_q8_attention")
+
+
+def fa_q8_step(layout: Q8Layout, cache: Q8Cache, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, out: torch.Tensor, ws: torch.Tensor,
+               stream=None) -> None:
+    """fa_q8_append of one token a row (k_new, v_new [B][H_kv][d]) then fa_q8_attention (q, out [B][H_q][d]) as one step."""
+    qs, ks, dt = (layout.batch, layout.n_q_heads, layout.head_dim), (layout.batch, layout.n_kv_heads, layout.head_dim), layout.torch_dtype
+    for t, shape in ((q, qs), (k_new, ks), (v_new, ks), (out, qs)):
+        if t.shape != shape or t.dtype != dt or not t.is_cuda or not t.is_contiguous():
+            raise ValueError("fa_q8_step: q, out [B][H_q][d] and k_new, v_new [B][H_kv][d] have to be contiguous tensors of the layout on the GPU")
+    status = lib().fa_q8_step(layout.ref(), cache._cref, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.numel(),
+                              _stream(stream))
+    if status:
+        _check(status, "fa_q8_step")
+
+
+def fa_q8_poll_status(cache: Q8Cache, stream=None) -> int:
+    return int(lib().fa_q8_poll_status(cache._cref, _stream(stream)))
