@@ -44,6 +44,7 @@ cudaError_t launch_q8_read(const Q8Dims&, const Q8Cache&, int fmt, int dtype, vo
                            cudaStream_t);
 // k_new / v_new non-null: a step (n_q = 1).
 size_t q8_attention_ws_bytes(const Q8Dims&, int n_q);
+bool q8_attention_fits(const Q8Dims&, int n_q);      // the units of work are counted in 32 bits
 cudaError_t launch_q8_attention(const Q8Dims&, const Q8Cache&, int fmt, int dtype, const void* q, int64_t sb, int64_t si, int64_t sg, void* out, int n_q,
                                 const void* k_new, const void* v_new, char* ws, cudaStream_t);
 

@@ -2,10 +2,10 @@
 //
 // A column is one (query, query head) of a KV head; a pass over the head's tokens serves 8 or 16 columns.  Scores and
 // outputs are formed transposed, S^T = K Q^T and O^T = V^T P^T (mma.sync m16n8k16, halves in, fp32 sums): the 16 rows are tokens,
-// then head dims, and no row is lost to padding of the few columns.  Both operands from the cache go straight from HBM to registers in
-// 16-byte pieces of token rows: the contraction over head dims may take them in any order as long as q follows it, and the rows
-// of O^T may be any dims, so that a lane's bytes are its own operand rows.  8-bit values are halves exactly; q is scaled by a
-// power of two per column, which makes its bf16 values halves exactly (fp32 q: a high and a low half, two products).
+// then head dims, and no row is lost to padding of the few columns.  The contraction over head dims may take them in any order as long as
+// q follows it, and the rows of O^T may be any dims: a lane reads its operand rows as 16 consecutive bytes of a token row.
+// 8-bit values are halves exactly; q is scaled by a power of two per column, which makes its bf16 values halves exactly (fp32 q: a high
+// and a low half, two products).
 //
 // Scales: a score is multiplied by its block's K scale.  The weight of a token in O is w = p sv 2^(m - m' + 15), sv its block's
 // V scale, m the column's running maximum of the scores, m' that of score + exponent of sv, both rounded up to whole numbers (of log2), so
@@ -13,9 +13,11 @@
 // or better; the sum of the p runs beside it in fp32.  The tail is the same with the power of two above its largest magnitude
 // in the place of the scale.
 //
-// Work: the (row, head, column tile) pairs have one unit for every 16 tokens in pages and one for the tail; the units of all pairs in a
-// line are cut into equal parts, one for each CTA, whatever the rows' lengths.  In a part, each of 8 warps takes every
-// 8th unit by itself with its loads one unit ahead; the warps join in shared memory, parts of one pair in the workspace, by the last CTA to finish, in a fixed order.
+// Work: a (row, head, column tile) pair has one unit for every 16 tokens in pages and one for the tail.  As long as there are fewer pairs than CTAs,
+// the pairs are cut into parts, as many in all as there are CTAs, no part over the end of a pair; with more pairs the units of
+// all pairs stand in a line that is cut into equal parts, whatever the rows' lengths.  In a part each of 8 warps takes every 8th
+// unit by itself, through a ring of its own in shared memory (cp.async, 16-byte chunks permuted so that the operand reads meet all banks);
+// the warps join in shared memory, the parts of a pair in the workspace, by the last CTA to finish, in the order of the tokens.
 // Bound by HBM for long rows, by the chain lengths - page - values - join for short ones.
 #include "fa_q8.cuh"
 
@@ -70,47 +72,62 @@ __device__ __forceinline__ uint32_t half2_rest(float a, float b, uint32_t hi) {
 __device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
 
 
-template <bool OWN>
-__device__ __forceinline__ uint4 ld16(const uint8_t* p) {
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there = true) {      // zeros if not there
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
     uint4 r;
-    if constexpr (OWN)                                     // written by this CTA
-        asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
-    else
-        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a) : "memory");
+    return r;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t a) {
+    uint2 r;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a) : "memory");
+    return r;
+}
+__device__ __forceinline__ float lds4(uint32_t a) {
+    float r;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(r) : "r"(a) : "memory");
     return r;
 }
 
-// The bytes of one unit (16 tokens of a page) that a lane (g, t) = (lane / 4, lane % 4) holds.
-template <int D, bool OWN = false>
-struct Raw {
-    static constexpr int kC = D / 64, kV = D == 64 ? 2 : D / 32;      // K chunks of 64 dims; words of a V row that a lane has
-    uint32_t k[kC][2][4];            // dims 64 c + 16 t .. + 15 of tokens g and g + 8
-    uint32_t v[4][kV];               // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9: dims 128 c + 16 g .. + 15 (D = 64: 8 g .. + 7)
-    float ks, vs;
-    __device__ __forceinline__ void load(const uint8_t* kp, const uint8_t* vp, int lane) {
-        const int g = lane >> 2, t = lane & 3;
-#pragma unroll
-        for (int c = 0; c < kC; ++c)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const uint4 x = ld16<OWN>(kp + (g + 8 * r) * D + 64 * c + 16 * t);
-                k[c][r][0] = x.x; k[c][r][1] = x.y; k[c][r][2] = x.z; k[c][r][3] = x.w;
-            }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const uint8_t* p = vp + (2 * t + (r & 1) + (r >> 1) * 8) * D;
-            if constexpr (D == 64) {
-                asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(v[r][0]), "=r"(v[r][1]) : "l"(p + 8 * g) : "memory");
-            } else {
-#pragma unroll
-                for (int c = 0; c < D / 128; ++c) {
-                    const uint4 x = ld16<OWN>(p + 128 * c + 16 * g);
-                    v[r][4 * c] = x.x; v[r][4 * c + 1] = x.y; v[r][4 * c + 2] = x.z; v[r][4 * c + 3] = x.w;
-                }
-            }
-        }
-    }
+// Ring of a warp.  A stage holds a unit (16 tokens) of pages: K rows, V rows, the two scales.  The tail's unit, in T, takes
+// kTail stages before the first unit of pages comes (none: fp32 rows of 256 dims, read from global memory instead).
+template <typename T, int D>
+struct Ring {
+    static constexpr int kBytes = 32 * D + 16;
+    static constexpr int kTail = sizeof(T) == 4 && D == 256 ? 0 : (int)sizeof(T);
+    static constexpr int kStages = kTail == 4 ? 5 : 3;
+    static constexpr int kFirst = kStages == 5 ? 4 : 2;              // stage of a part's first unit
+    static_assert(kTail * 32 * D >= (kTail ? 32 * D * (int)sizeof(T) : 0), "the tail's unit fits");
 };
+// Chunk (16 bytes) `c` of row `r` of a unit: the chunks of a 128-byte line are permuted by a key that differs between the rows that a read meets.
+template <int D>
+__device__ __forceinline__ int unit_offset(int r, int c) {
+    if constexpr (D == 64) return (r >> 1) * 128 + (((((r & 1) << 2) | c) ^ (r & 6)) << 4);
+    else return r * D + (((c & ~7) | ((c ^ r) & 7)) << 4);
+}
+// First dim of the 16 that lane t of a quad takes of a K row (and of q) as its `c`-th piece.
+template <int D>
+__device__ __forceinline__ int k_dim(int c, int t) { return D == 64 ? 16 * t : 128 * (c >> 1) + 32 * t + 16 * (c & 1); }
+
+template <int D>
+__device__ __forceinline__ void issue_unit(uint32_t stage, const uint8_t* kp, const uint8_t* vp, const float* ks, const float* vs, int lane) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+        const int l = i * 32 + lane, off = unit_offset<D>(l / (D / 16), l % (D / 16));
+        cp16(stage + off, kp + 16 * l);
+        cp16(stage + 16 * D + off, vp + 16 * l);
+    }
+    if (lane < 2) cp4(stage + 32 * D + 4 * lane, lane ? vs : ks);
+}
 
 // The columns of a segment as a warp holds them.
 template <typename T, int D, int NT>
@@ -189,26 +206,48 @@ struct Columns {
     }
 };
 
-template <typename T, int FMT, int D, int NT, bool OWN>
-__device__ __forceinline__ void unit_of_page(Columns<T, D, NT>& C, const Raw<D, OWN>& r, int tok, bool edge) {
+template <typename T, int FMT, int D, int NT>
+__device__ __forceinline__ void unit_of_page(Columns<T, D, NT>& C, uint32_t stage, int tok, bool edge, int lane) {
+    const int g = lane >> 2, t = lane & 3;
     float s[NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c)
+    for (int c = 0; c < D / 64; ++c) {
+        const uint4 x4 = lds16(stage + unit_offset<D>(g, k_dim<D>(c, t) >> 4)), y4 = lds16(stage + unit_offset<D>(g + 8, k_dim<D>(c, t) >> 4));
+        const uint32_t xw[4] = {x4.x, x4.y, x4.z, x4.w}, yw[4] = {y4.x, y4.y, y4.z, y4.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t x = q8_flip<FMT>(r.k[c][0][j]), y = q8_flip<FMT>(r.k[c][1][j]);
+            const uint32_t x = q8_flip<FMT>(xw[j]), y = q8_flip<FMT>(yw[j]);
             C.mma_s(s, 4 * c + j, q8_halves<FMT>(x, 0), q8_halves<FMT>(y, 0), q8_halves<FMT>(x, 1), q8_halves<FMT>(y, 1));
         }
+    }
     uint32_t w[NT][2], wl[NT][2];
-    C.weights(s, r.ks, r.vs, tok, edge, w, wl);
+    C.weights(s, lds4(stage + 32 * D), lds4(stage + 32 * D + 4), tok, edge, w, wl);
+    const uint32_t vst = stage + 16 * D;
 #pragma unroll
-    for (int i = 0; i < Raw<D>::kV; ++i) {
-        const uint32_t a = q8_flip<FMT>(r.v[0][i]), b = q8_flip<FMT>(r.v[1][i]), c = q8_flip<FMT>(r.v[2][i]), d = q8_flip<FMT>(r.v[3][i]);
-        const uint32_t ab0 = __byte_perm(a, b, 0x5140), ab1 = __byte_perm(a, b, 0x7362), cd0 = __byte_perm(c, d, 0x5140), cd1 = __byte_perm(c, d, 0x7362);
-        C.mma_o(2 * i, w, wl, q8_halves<FMT>(ab0, 0), q8_halves<FMT>(ab0, 1), q8_halves<FMT>(cd0, 0), q8_halves<FMT>(cd0, 1));
-        C.mma_o(2 * i + 1, w, wl, q8_halves<FMT>(ab1, 0), q8_halves<FMT>(ab1, 1), q8_halves<FMT>(cd1, 0), q8_halves<FMT>(cd1, 1));
+    for (int c = 0; c < (D == 64 ? 1 : D / 128); ++c) {
+        constexpr int kW = D == 64 ? 2 : 4;
+        uint32_t v[4][kW];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = 2 * t + (r & 1) + (r >> 1) * 8;
+            if constexpr (D == 64) {
+                const uint2 x = lds8(vst + unit_offset<D>(row, g >> 1) + 8 * (g & 1));
+                v[r][0] = x.x; v[r][1] = x.y;
+            } else {
+                const uint4 x = lds16(vst + unit_offset<D>(row, 8 * c + g));
+                v[r][0] = x.x; v[r][1] = x.y; v[r][2] = x.z; v[r][3] = x.w;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+            const uint32_t p = q8_flip<FMT>(v[0][i]), q = q8_flip<FMT>(v[1][i]), r = q8_flip<FMT>(v[2][i]), u = q8_flip<FMT>(v[3][i]);
+            const uint32_t ab0 = __byte_perm(p, q, 0x5140), ab1 = __byte_perm(p, q, 0x7362), cd0 = __byte_perm(r, u, 0x5140), cd1 = __byte_perm(r, u, 0x7362);
+            const int mt = 2 * kW * c + 2 * i;
+            C.mma_o(mt, w, wl, q8_halves<FMT>(ab0, 0), q8_halves<FMT>(ab0, 1), q8_halves<FMT>(cd0, 0), q8_halves<FMT>(cd0, 1));
+            C.mma_o(mt + 1, w, wl, q8_halves<FMT>(ab1, 0), q8_halves<FMT>(ab1, 1), q8_halves<FMT>(cd1, 0), q8_halves<FMT>(cd1, 1));
+        }
     }
 }
 
@@ -225,35 +264,55 @@ __device__ __forceinline__ uint32_t pair_of2(const Vec16<T>& u, const Vec16<T>& 
     const uint32_t h = half2_of(a, b);
     return rest ? half2_rest(a, b, h) : h;
 }
-// Sixteen elements of the tail that this kernel may have written; nothing behind the row's last token is read.
+// The tail of a KV head as a warp meets it.  `fresh`: the row that a step pushes comes from k_new / v_new (another warp may be writing it).
 template <typename T>
-__device__ __forceinline__ void load_own16(Vec16<T>& v, const T* p, bool there) {
-    if (!there) { v.zero(); return; }
-    uint4 x[sizeof(T)];
+struct Tail {
+    const T *k, *v, *k_new, *v_new;
+    int here, fresh;                 // tokens in the tail; the row that is pushed, -1 without one
+    uint32_t kmax, vmax;
+    __device__ __forceinline__ const T* row(int side, int r, int D) const { return r == fresh ? (side ? v_new : k_new) : (side ? v : k) + (size_t)r * D; }
+};
+template <typename T, int D>
+__device__ __forceinline__ void issue_tail(uint32_t ring, const Tail<T>& tl, int sub, int lane) {
+    constexpr int kChunks = D * (int)sizeof(T) / 16;      // of a row
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) x[i] = ld16<true>(reinterpret_cast<const uint8_t*>(p) + 16 * i);
-    memcpy(&v, x, sizeof(v));
+    for (int i = 0; i < 16 * kChunks / 32; ++i) {
+        const int l = i * 32 + lane, r = sub * kUnit + l / kChunks, e = (l % kChunks) * (16 / (int)sizeof(T));
+        const bool there = r < tl.here;
+        cp16(ring + 16 * l, tl.row(0, there ? r : 0, D) + e, there);
+        cp16(ring + 16 * (l + 16 * kChunks), tl.row(1, there ? r : 0, D) + e, there);
+    }
 }
 
-// Unit `sub` of the tail: `here` tokens of the row are in the tail, which starts at token `first`.
+// Unit `sub` of the tail, which starts at token `first` of the row; from the ring, or from global memory.
 template <typename T, int D, int NT>
-__device__ __forceinline__ void unit_of_tail(Columns<T, D, NT>& C, const T* kt, const T* vt, uint32_t kmax, uint32_t vmax, int sub, int here, int first,
-                                             int lane) {
-    constexpr bool kF32 = sizeof(T) == 4;
+__device__ __forceinline__ void unit_of_tail(Columns<T, D, NT>& C, const Tail<T>& tl, uint32_t ring, int sub, int first, int lane) {
+    constexpr bool kF32 = sizeof(T) == 4, kRing = Ring<T, D>::kTail != 0;
     const int g = lane >> 2, t = lane & 3, row0 = sub * kUnit;
     // the power of two that brings the largest magnitude to 2^13 .. 2^14, where halves hold the values next to it in full
-    const bool kbad = kmax >= 0x7f800000u, vbad = vmax >= 0x7f800000u;
-    const int ek = max((int)(kmax >> 23) - 127, -100), evt = max((int)(vmax >> 23) - 127, -100);
-    const float kf = kbad ? 0.f : pow2i(13 - ek), vf = vbad ? 0.f : pow2i(13 - evt);
+    const bool kbad = tl.kmax >= 0x7f800000u, vbad = tl.vmax >= 0x7f800000u;
+    const int ek = max((int)(tl.kmax >> 23) - 127, -100), evt = max((int)(tl.vmax >> 23) - 127, -100);
+    const float kf = pow2i(13 - ek), vf = pow2i(13 - evt);
     const float ks = kbad ? __uint_as_float(0x7fc00000u) : pow2i(ek - 13), vs = vbad ? __uint_as_float(0x7fc00000u) : pow2i(evt - 13);
+    auto get = [&](Vec16<T>& x, int side, int r, int e) {            // 16 elements of row r of the unit; zeros behind the row's last token
+        if ((side ? vbad : kbad) || row0 + r >= tl.here) { x.zero(); return; }
+        if constexpr (kRing) {
+            uint4 w[sizeof(T)];
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T); ++i) w[i] = lds16(ring + (16 * side + r) * D * (int)sizeof(T) + e * (int)sizeof(T) + 16 * i);
+            memcpy(&x, w, sizeof(x));
+        } else {
+            x.load(tl.row(side, row0 + r, D) + e);
+        }
+    };
     float s[NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
         Vec16<T> x, y;
-        load_own16(x, kt + (size_t)(row0 + g) * D + 64 * c + 16 * t, row0 + g < here && !kbad);
-        load_own16(y, kt + (size_t)(row0 + g + 8) * D + 64 * c + 16 * t, row0 + g + 8 < here && !kbad);
+        get(x, 0, g, k_dim<D>(c, t));
+        get(y, 0, g + 8, k_dim<D>(c, t));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             C.mma_s(s, 4 * c + j, pair_of(x, 4 * j, kf, false), pair_of(y, 4 * j, kf, false), pair_of(x, 4 * j + 2, kf, false), pair_of(y, 4 * j + 2, kf, false));
@@ -267,11 +326,7 @@ __device__ __forceinline__ void unit_of_tail(Columns<T, D, NT>& C, const T* kt, 
     for (int c = 0; c < (D == 64 ? 1 : D / 128); ++c) {
         Vec16<T> v[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = row0 + 2 * t + (r & 1) + (r >> 1) * 8;
-            const int e = D == 64 ? (g >> 1) * 16 : 128 * c + 16 * g;
-            load_own16(v[r], vt + (size_t)row * D + e, row < here && !vbad);
-        }
+        for (int r = 0; r < 4; ++r) get(v[r], 1, 2 * t + (r & 1) + (r >> 1) * 8, D == 64 ? (g >> 1) * 16 : 128 * c + 16 * g);
 #pragma unroll
         for (int i = 0; i < (D == 64 ? 4 : 8); ++i) {
             // (D = 64: a lane's 8 dims are one half of its 16)
@@ -322,43 +377,41 @@ __device__ __forceinline__ RowPlan row_plan(const AttnArgs& a, int b, bool tell)
     return r;
 }
 
-// The push of a step for one KV head, by the CTA that has the tail unit: the token into the tail; if that completes the
-// block, its page.  mx: largest magnitudes of the tail's K and V (as bits) for all threads.
-template <typename T, int FMT, int D>
-__device__ __forceinline__ void push_token(const AttnArgs& a, int b, int h, int len, T* kt, T* vt, uint32_t* mx) {
-    const Q8Dims& s = a.s;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int r = len & (s.blk - 1);
-    float* amax = a.c.tail_amax + ((size_t)b * s.H + h) * 2;
-    if (warp < 2) {                                        // K by warp 0, V by warp 1
-        const T* src = reinterpret_cast<const T*>(warp ? a.v_new : a.k_new) + ((size_t)b * s.H + h) * D;
-        T* dst = (warp ? vt : kt) + (size_t)r * D;
-        uint32_t m = 0;
-        if (lane < D / 16) {
-            Vec16<T> v;
-            v.load(src + 16 * lane);
-            v.store(dst + 16 * lane);
-            m = v.amax_bits();
-        }
-        m = __reduce_max_sync(0xffffffffu, m);
-        if (lane == 0) {
-            if (r > 0) m = max(m, __float_as_uint(amax[warp]));
-            amax[warp] = __uint_as_float(m);
-            mx[warp] = m;
-        }
+// The push of a step for one KV head, by the CTA that has the tail unit.  Largest magnitudes with the pushed token, by every warp for itself:
+template <typename T, int D>
+__device__ __forceinline__ void push_amax(const AttnArgs& a, int b, int h, int r, int lane, uint32_t& km, uint32_t& vm) {
+    const size_t bh = (size_t)b * a.s.H + h;
+    uint32_t m = 0;
+    if ((lane & 15) < D / 16) {                            // K by lanes 0 .., V by lanes 16 ..
+        Vec16<T> v;
+        v.load(reinterpret_cast<const T*>(lane < 16 ? a.k_new : a.v_new) + bh * D + 16 * (lane & 15));
+        m = v.amax_bits();
     }
-    __syncthreads();
-    if (r + 1 < s.blk) return;
-    const int page = a.c.table[(size_t)b * s.nb + (len >> s.lb)];      // (in range: row_plan)
-    const size_t ph = (size_t)page * s.H + h;
-    const int nvec = s.blk * (D / 16);
+    if (r > 0 && (lane & 15) == 0) m = max(m, __float_as_uint(a.c.tail_amax[bh * 2 + (lane >> 4)]));
+    km = __reduce_max_sync(0xffffffffu, lane < 16 ? m : 0u);
+    vm = __reduce_max_sync(0xffffffffu, lane < 16 ? 0u : m);
+}
+// ... the token's rows, by one warp (its magnitudes are written when all warps have read the old ones) ...
+template <typename T, int D>
+__device__ __forceinline__ void push_rows(const AttnArgs& a, int b, int h, int r, T* kt, T* vt, int lane) {
+    if ((lane & 15) >= D / 16) return;
+    Vec16<T> v;
+    v.load(reinterpret_cast<const T*>(lane < 16 ? a.k_new : a.v_new) + ((size_t)b * a.s.H + h) * D + 16 * (lane & 15));
+    v.store((lane < 16 ? kt : vt) + (size_t)r * D + 16 * (lane & 15));
+}
+// ... and the block's page, if the token completes it, by the whole CTA (the rows are written, all threads are past a barrier).
+template <typename T, int FMT, int D>
+__device__ __forceinline__ void push_page(const AttnArgs& a, size_t ph, const T* kt, const T* vt, uint32_t km, uint32_t vm) {
+    const int nvec = a.s.blk * (D / 16);
 #pragma unroll 1
     for (int side = 0; side < 2; ++side) {
-        const Q8Round<FMT, T> to(mx[side]);
-        uint8_t* out = (side ? a.c.v_pages : a.c.k_pages) + ph * (size_t)(s.blk * D);
-        for (int i = tid; i < nvec; i += kThreads) {
+        const uint32_t m = side ? vm : km;
+        const Q8Round<FMT, T> to(m);
+        uint8_t* out = (side ? a.c.v_pages : a.c.k_pages) + ph * (size_t)(a.s.blk * D);
+#pragma unroll 1
+        for (int i = threadIdx.x; i < nvec; i += kThreads) {
             Vec16<T> v;
-            load_own16(v, (side ? vt : kt) + (size_t)i * 16, true);
+            v.load((side ? vt : kt) + (size_t)i * 16);
             uint4 o;
             o.x = to.pack(v.at(0), v.at(1), v.at(2), v.at(3));
             o.y = to.pack(v.at(4), v.at(5), v.at(6), v.at(7));
@@ -366,9 +419,8 @@ __device__ __forceinline__ void push_token(const AttnArgs& a, int b, int h, int 
             o.w = to.pack(v.at(12), v.at(13), v.at(14), v.at(15));
             *reinterpret_cast<uint4*>(out + (size_t)i * 16) = o;
         }
-        if (tid == 0) (side ? a.c.v_scale : a.c.k_scale)[ph] = Q8Round<FMT, T>::scale(mx[side]);
+        if (threadIdx.x == 0) (side ? a.c.v_scale : a.c.k_scale)[ph] = Q8Round<FMT, T>::scale(m);
     }
-    __syncthreads();
 }
 
 template <typename T>
@@ -390,85 +442,235 @@ __device__ __forceinline__ float4 finish(float4 o, float m, float mp, float l) {
     return make_float4(o.x * r * f * f2, o.y * r * f * f2, o.z * r * f * f2, o.w * r * f * f2);
 }
 
+// The parts of one pair, in the order of the tokens: a warp per column finds the maxima and every part's factor, then each
+// thread sums four dims of a column over its share of the parts (a few shares where the columns are few), with loads of
+// eight parts in flight.
+template <typename T, int D, int kCols, typename Store>
+__device__ __forceinline__ void join_parts(const float* part, int cta0, bool line, int n_seg, int n_col, float* sm, float (&ml)[3][kWarps][kCols], const Store& store) {
+    constexpr int kPitch = D + 4, kChunk = 128;            // parts whose factors lie in shared memory at a time: [column][kChunk]
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    auto at = [&](int j, int col) { return part + ((size_t)2 * (cta0 + j) + (line && j == 0 ? 1 : 0)) * kCols * kPitch + col * kPitch; };
+    for (int col = warp; col < n_col; col += kWarps) {
+        float m = kNegBig, mp = kNegBig, l = 0.f;
+        for (int j = lane; j < n_seg; j += 32) {
+            const float4 hd = __ldcg(reinterpret_cast<const float4*>(at(j, col) + D));
+            const float mn = fmaxf(m, hd.x);
+            l = l * pow2_down(m, mn) + hd.z * pow2_down(hd.x, mn);
+            m = mn;
+            mp = fmaxf(mp, hd.y);
+        }
+        const float mx = warp_max(m);
+        mp = warp_max(mp);
+        l = warp_sum(l * pow2_down(m, mx));
+        if (lane == 0) { ml[0][0][col] = mx; ml[1][0][col] = mp; ml[2][0][col] = l; }
+    }
+    const int slots = n_col * (D / 4), shares = slots <= kThreads / 2 ? kThreads / slots : 1;
+    float* fac = sm;                                       // [kCols][kChunk]
+    float4* acc = reinterpret_cast<float4*>(sm + kCols * kChunk);      // [shares - 1][slots]
+    for (int i0 = 0; i0 < slots; i0 += kThreads) {
+        const int i = shares > 1 ? tid % slots : i0 + tid, share = shares > 1 ? tid / slots : 0;
+        const bool on = i < slots && share < shares;
+        const int col = i / (D / 4), e = (i % (D / 4)) * 4;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int j0 = 0; j0 < n_seg; j0 += kChunk) {
+            const int n = min(kChunk, n_seg - j0);
+            __syncthreads();
+            for (int k = tid; k < n_col * kChunk; k += kThreads) {
+                const int c = k / kChunk, j = k % kChunk;
+                if (j < n) fac[k] = pow2_down(__ldcg(at(j0 + j, c) + D + 1), ml[1][0][c]);
+            }
+            __syncthreads();
+            if (!on) continue;
+            for (int j = share; j < n; j += 8 * shares) {
+                float4 x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (j + k * shares < n) x[k] = __ldcg(reinterpret_cast<const float4*>(at(j0 + j + k * shares, col) + e));
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (j + k * shares < n) {
+                        const float f = fac[col * kChunk + j + k * shares];
+                        o.x = fmaf(x[k].x, f, o.x); o.y = fmaf(x[k].y, f, o.y); o.z = fmaf(x[k].z, f, o.z); o.w = fmaf(x[k].w, f, o.w);
+                    }
+            }
+        }
+        if (shares > 1) {
+            if (on && share > 0) acc[(share - 1) * slots + i] = o;
+            __syncthreads();
+            if (share == 0)
+                for (int k = 1; k < shares; ++k) {
+                    const float4 x = acc[(k - 1) * slots + i];
+                    o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+                }
+        }
+        if (on && share == 0) store(col, e, o, ml[0][0][col], ml[1][0][col], ml[2][0][col]);
+    }
+}
+
 template <typename T, int FMT, int D, int NT, bool STEP>
 __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 2 ? 2 : 1) q8_attn_kernel(const AttnArgs a) {
     constexpr bool kF32 = sizeof(T) == 4;
     constexpr int kCols = 8 * NT, kMt = D / 16, kPitch = D + 4;
+    using R = Ring<T, D>;
     extern __shared__ float4 smem4[];
-    float* osm = reinterpret_cast<float*>(smem4);          // [warps][columns][pitch]
+    float* osm = reinterpret_cast<float*>(smem4);          // the rings; then [warps][columns][pitch]; then a join's factors and shares
     __shared__ float ml[3][kWarps][kCols];
-    __shared__ long long plan_s[3];                        // units of all pairs; the first row of this CTA's part, its units before
-    __shared__ uint32_t mx[2];
     __shared__ int last_s;
     const Q8Dims& s = a.s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int per_row = s.H * a.n_ct;
+    const unsigned per_row = (unsigned)(s.H * a.n_ct), ctas = gridDim.x;
+    const uint32_t ring = smem_addr(smem4) + (uint32_t)(warp * R::kStages * R::kBytes);
 
-    // ---- the part of the line of units that is this CTA's ----
-    if (warp == 0) {
-        long long total = 0;
-        for (int b0 = 0; b0 < s.B; b0 += 32) {
-            int u = b0 + lane < s.B ? row_plan<STEP>(a, b0 + lane, blockIdx.x == 0).units : 0;
-            long long v = (long long)u * per_row;
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-            total += v;
-        }
-        if (lane == 0) plan_s[0] = total;
+    // ---- this CTA's part, found by every warp for itself; lanes hold 32 rows at a time ----
+    RowPlan mine = {0, 0, 0, false};
+    auto rows_from = [&](int b0, bool tell) {              // (up to 32 rows are loaded once)
+        if (s.B <= 32 && !tell) return;
+        mine = RowPlan{0, 0, 0, false};
+        if (b0 + lane < s.B) mine = row_plan<STEP>(a, b0 + lane, tell && blockIdx.x == 0 && warp == 0);
+    };
+    unsigned total = 0, pairs = 0, most = 0;
+    for (int b0 = 0; b0 < s.B; b0 += 32) {
+        rows_from(b0, true);
+        total += __reduce_add_sync(0xffffffffu, (unsigned)mine.units * per_row);
+        pairs += (unsigned)__popc(__ballot_sync(0xffffffffu, mine.units > 0)) * per_row;
+        most = max(most, __reduce_max_sync(0xffffffffu, (unsigned)mine.units));
     }
-    __syncthreads();
-    const long long total = plan_s[0];
-    long long per = (total + gridDim.x - 1) / gridDim.x;
-    if (per < kWarps) per = kWarps;                        // a unit for each warp at least
-    long long u0 = per * blockIdx.x;
-    const long long u1 = u0 + per < total ? u0 + per : total;
-    if (warp == 0) {
-        long long before = 0;
+    // Fewer pairs than CTAs: the smallest parts (of 8 units at least, one for each warp) that are no more than the CTAs.
+    // Each lane tries a size, 2^(1/10) apart from total / CTAs on, the last one that of the longest pair.
+    const bool line = pairs > ctas;
+    unsigned per = max((total + ctas - 1) / ctas, (unsigned)kWarps);
+    if (!line) {
+        const unsigned size = lane == 31 ? max(most, per) : (unsigned)ceilf((float)per * exp2f(0.1f * (float)lane));
+        unsigned parts = 0;
         for (int b0 = 0; b0 < s.B; b0 += 32) {
-            int u = b0 + lane < s.B ? row_plan<STEP>(a, b0 + lane, false).units : 0;
-            const long long mine = (long long)u * per_row;
-            long long v = mine;
+            rows_from(b0, false);
+            for (int i = 0; i < min(32, s.B - b0); ++i) parts += ((unsigned)__shfl_sync(0xffffffffu, mine.units, i) + size - 1) / size * per_row;
+        }
+        per = __shfl_sync(0xffffffffu, size, __ffs(__ballot_sync(0xffffffffu, parts <= ctas)) - 1);
+    }
+    unsigned u0 = line ? min(per * blockIdx.x, total) : blockIdx.x;  // in units of the line, or in parts
+    const unsigned u1 = line ? min(u0 + per, total) : blockIdx.x + 1;
+    unsigned base = 0;                                               // units (parts) in front of row b
+    int b = 0;
+    RowPlan row = {0, 0, 0, false};
+    auto of_row = [&](int units) { return (line ? (unsigned)units : ((unsigned)units + per - 1) / per) * per_row; };
+    {
+        bool found = false;
+        unsigned before = 0;
+        for (int b0 = 0; b0 < s.B && !found; b0 += 32) {
+            rows_from(b0, false);
+            const unsigned n = of_row(mine.units);
+            unsigned v = n;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
-                const long long w = __shfl_up_sync(0xffffffffu, v, d);
+                const unsigned w = __shfl_up_sync(0xffffffffu, v, d);
                 if (lane >= d) v += w;
             }
             const unsigned hit = __ballot_sync(0xffffffffu, before + v > u0);
             if (hit) {
                 const int src = __ffs(hit) - 1;
-                const long long row_before = before + __shfl_sync(0xffffffffu, v - mine, src);
-                if (lane == 0) { plan_s[1] = b0 + src; plan_s[2] = row_before; }
-                break;
+                b = b0 + src;
+                base = before + __shfl_sync(0xffffffffu, v - n, src);
+                row.len = __shfl_sync(0xffffffffu, mine.len, src);
+                row.first = __shfl_sync(0xffffffffu, mine.first, src);
+                row.units = __shfl_sync(0xffffffffu, mine.units, src);
+                row.push = __shfl_sync(0xffffffffu, (int)mine.push, src);
+                found = true;
             }
             before += __shfl_sync(0xffffffffu, v, 31);
         }
+        if (!found) u0 = u1;                               // nothing left for this CTA
     }
-    // rows without a token: zeros
-    for (int b = blockIdx.x; b < s.B; b += gridDim.x)
-        if (row_plan<STEP>(a, b, false).units == 0) {
-            const int n4 = a.n_q * s.Hq * D / 4;
-            T* o = reinterpret_cast<T*>(a.out) + (size_t)b * a.n_q * s.Hq * D;
-            for (int i = tid; i < n4; i += kThreads) st4(o + (size_t)i * 4, make_float4(0.f, 0.f, 0.f, 0.f));
-        }
-    __syncthreads();
-    int b = (int)plan_s[1];
-    long long base = plan_s[2];
+
     while (u0 < u1) {
-        RowPlan row = row_plan<STEP>(a, b, false);
-        const long long row_units = (long long)row.units * per_row;
-        if (u0 >= base + row_units) { base += row_units; ++b; continue; }
-        const int pair = (int)((u0 - base) / row.units);
+        if (u0 >= base + of_row(row.units)) {              // (a line only)
+            base += of_row(row.units);
+            row = row_plan<STEP>(a, ++b, false);
+            continue;
+        }
+        int pair, s0, s1, cta0, n_seg;
+        if (line) {
+            pair = (int)((u0 - base) / (unsigned)row.units);
+            const unsigned pair0 = base + (unsigned)pair * (unsigned)row.units;
+            s0 = (int)(u0 - pair0);
+            s1 = (int)min(u1 - pair0, (unsigned)row.units);
+            u0 = pair0 + s1;
+            cta0 = (int)(pair0 / per);
+            n_seg = (int)((pair0 + row.units - 1) / per) - cta0 + 1;
+        } else {
+            n_seg = (int)(((unsigned)row.units + per - 1) / per);
+            pair = (int)((u0 - base) / (unsigned)n_seg);
+            const int j = (int)(u0 - base) - pair * n_seg, even = (row.units + n_seg - 1) / n_seg;
+            s0 = min(j * even, row.units);
+            s1 = min(s0 + even, row.units);
+            cta0 = (int)u0 - j;
+            ++u0;
+        }
         const int h = pair / a.n_ct, ct = pair % a.n_ct;
-        const long long pair0 = base + (long long)pair * row.units;
-        const int s0 = (int)(u0 - pair0), s1 = (int)(u1 - pair0 < row.units ? u1 - pair0 : row.units);
-        u0 = pair0 + s1;
         const int paged = row.first / kUnit;
         T* kt = reinterpret_cast<T*>(a.c.k_tail) + ((size_t)b * s.H + h) * (size_t)s.blk * D;
         T* vt = reinterpret_cast<T*>(a.c.v_tail) + ((size_t)b * s.H + h) * (size_t)s.blk * D;
+        const int32_t* table = a.c.table + (size_t)b * s.nb;
+        const int lu = s.lb - 4;                           // units of a block
+        const int seen = row.len - a.n_q + 1 + min(a.n_q - 1, (ct * kCols + kCols - 1) / s.G);   // tokens that some column of the tile sees
+        const int sure = row.len - a.n_q + 1 + ct * kCols / s.G;                                 // ... that all columns see
+        const int stop = min(min(s1, paged), (seen + kUnit - 1) / kUnit);
+
+        // ---- loads: the tail's unit, the first unit in pages ----
+        auto page_of = [&](int u) {
+            if (u >= stop) return -1;
+            const int p = table[u >> lu];
+            if (p >= 0 && p < s.n_pages) return p;
+            if (lane == 0) q8_report(a.c.status, FA_ERR_INDEX);
+            return -1;
+        };
+        auto issue = [&](int stage, int u, int page) {
+            if (page >= 0) {
+                const size_t ph = (size_t)page * s.H + h;
+                const size_t at = (ph * (size_t)s.blk + (size_t)(u & ((1 << lu) - 1)) * kUnit) * D;
+                issue_unit<D>(ring + (uint32_t)(stage * R::kBytes), a.c.k_pages + at, a.c.v_pages + at, a.c.k_scale + ph, a.c.v_scale + ph, lane);
+            }
+            cp_commit();
+        };
+        constexpr int kAhead = R::kStages - 1;
+        int u = s0 + warp, pages[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) pages[i] = page_of(u + i * kWarps);
+        Tail<T> tl = {kt, vt, nullptr, nullptr, row.len - row.first, -1, 0u, 0u};
+        bool tail = s1 > paged && row.first + warp * kUnit < min(row.len, seen);       // this warp has a unit of the tail
+        bool whole = false;                                                             // which a step has just completed
+        if (s1 > paged) {
+            const size_t bh = (size_t)b * s.H + h;
+            if (STEP && row.push) {
+                push_amax<T, D>(a, b, h, tl.here - 1, lane, tl.kmax, tl.vmax);
+                if (warp == kWarps - 1) push_rows<T, D>(a, b, h, tl.here - 1, kt, vt, lane);
+                tl.fresh = tl.here - 1;
+                tl.k_new = reinterpret_cast<const T*>(a.k_new) + bh * D;
+                tl.v_new = reinterpret_cast<const T*>(a.v_new) + bh * D;
+                __syncthreads();
+                if (tid < 2) a.c.tail_amax[bh * 2 + tid] = __uint_as_float(tid ? tl.vmax : tl.kmax);
+                if (tl.here == s.blk) {
+                    const size_t ph = (size_t)table[row.first >> s.lb] * s.H + h;       // (in range: row_plan)
+                    push_page<T, FMT, D>(a, ph, kt, vt, tl.kmax, tl.vmax);
+                    __threadfence();
+                    __syncthreads();
+                    whole = true;
+                    if (tail) {
+                        const size_t at = (ph * (size_t)s.blk + (size_t)warp * kUnit) * D;
+                        issue_unit<D>(ring, a.c.k_pages + at, a.c.v_pages + at, a.c.k_scale + ph, a.c.v_scale + ph, lane);
+                    }
+                }
+            } else {
+                tl.kmax = __float_as_uint(a.c.tail_amax[bh * 2]);
+                tl.vmax = __float_as_uint(a.c.tail_amax[bh * 2 + 1]);
+            }
+            if (tail && !whole && R::kTail) issue_tail<T, D>(ring, tl, warp, lane);
+        }
+        cp_commit();
+        issue(R::kFirst, u, pages[0]);
 
         // ---- columns ----
         Columns<T, D, NT> C;
-        int seen = 0;                                      // tokens that some column of the tile sees
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int col = ct * kCols + nt * 8 + g, qi = col / s.G, gq = col % s.G;
@@ -478,7 +680,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
             uint32_t mxq = 0;
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) {
-                if (there) v[c].load(qp + 64 * c + 16 * t);
+                if (there) v[c].load(qp + k_dim<D>(c, t));
                 else v[c].zero();
                 mxq = max(mxq, v[c].amax_bits());
             }
@@ -504,73 +706,37 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
                 C.m[nt][k] = C.mp[nt][k] = kNegBig;
                 C.l[nt][k] = 0.f;
             }
-            seen = max(seen, __reduce_max_sync(0xffffffffu, lastq) + 1);
 #pragma unroll
             for (int i = 0; i < kMt; ++i) C.o[nt][i][0] = C.o[nt][i][1] = C.o[nt][i][2] = C.o[nt][i][3] = 0.f;
         }
-        int sure = row.len - a.n_q + 1 + ct * kCols / s.G;  // tokens that all columns of the tile see
-        // ---- units in pages ----
-        {
-            const int32_t* table = a.c.table + (size_t)b * s.nb;
-            const int stop = min(min(s1, paged), (seen + kUnit - 1) / kUnit);
-            const int lu = s.lb - 4;                        // units of a block
-            auto page_of = [&](int u) {
-                if (u >= stop) return -1;
-                const int p = table[u >> lu];
-                if (p >= 0 && p < s.n_pages) return p;
-                if (lane == 0) q8_report(a.c.status, FA_ERR_INDEX);
-                return -1;
-            };
-            auto fetch = [&](Raw<D>& r, int u, int page) {
-                if (page < 0) return;
-                const size_t ph = (size_t)page * s.H + h;
-                const size_t at = (ph * (size_t)s.blk + (size_t)(u & ((1 << lu) - 1)) * kUnit) * D;
-                r.load(a.c.k_pages + at, a.c.v_pages + at, lane);
-                r.ks = __ldg(a.c.k_scale + ph);
-                r.vs = __ldg(a.c.v_scale + ph);
-            };
-            int u = s0 + warp;
-            int page = page_of(u), page1 = page_of(u + kWarps);
-            Raw<D> cur, nxt;
-            fetch(cur, u, page);
-            for (; u < stop; u += kWarps) {
-                const int page2 = page_of(u + 2 * kWarps);
-                fetch(nxt, u + kWarps, page1);
-                if (page >= 0) unit_of_page<T, FMT, D, NT, false>(C, cur, u * kUnit + g, u * kUnit + kUnit > sure);
-                cur = nxt;
-                page = page1;
-                page1 = page2;
-            }
-        }
         // ---- the tail ----
-        if (s1 > paged) {
-            const int here = row.len - row.first;
-            uint32_t km, vm;
-            if constexpr (STEP) {
-                if (row.push) push_token<T, FMT, D>(a, b, h, row.len - 1, kt, vt, mx);
-            }
-            if (STEP && row.push) {
-                km = mx[0];
-                vm = mx[1];
-            } else {
-                const float* am = a.c.tail_amax + ((size_t)b * s.H + h) * 2;
-                km = __float_as_uint(am[0]);
-                vm = __float_as_uint(am[1]);
-            }
-            if (warp * kUnit < here && row.first + warp * kUnit < seen) {
-                if (STEP && here == s.blk) {               // complete with this token
-                    const int page = a.c.table[(size_t)b * s.nb + (row.first >> s.lb)];
-                    const size_t ph = (size_t)page * s.H + h, at = (ph * (size_t)s.blk + (size_t)warp * kUnit) * D;
-                    Raw<D, true> r;
-                    r.load(a.c.k_pages + at, a.c.v_pages + at, lane);
-                    r.ks = Q8Round<FMT, T>::scale(km);
-                    r.vs = Q8Round<FMT, T>::scale(vm);
-                    unit_of_page<T, FMT, D, NT, true>(C, r, row.first + warp * kUnit + g, true);
-                } else {
-                    unit_of_tail<T, D, NT>(C, kt, vt, km, vm, warp, here, row.first, lane);
-                }
-            }
+        if (tail) {
+            cp_wait<1>();
+            __syncwarp();
+            if (STEP && whole) unit_of_page<T, FMT, D, NT>(C, ring, row.first + warp * kUnit + g, true, lane);
+            else unit_of_tail<T, D, NT>(C, tl, ring, warp, row.first, lane);
+            __syncwarp();
         }
+        // ---- units in pages ----
+#pragma unroll
+        for (int i = 1; i < kAhead; ++i) issue((R::kFirst + i) % R::kStages, u + i * kWarps, pages[i]);
+        int stage = R::kFirst, page1 = page_of(u + kAhead * kWarps);
+#pragma unroll 1
+        for (; u < stop; u += kWarps) {
+            cp_wait<kAhead - 1>();
+            __syncwarp();
+            const int page2 = page_of(u + (kAhead + 1) * kWarps);
+            issue(stage == 0 ? R::kStages - 1 : stage - 1, u + kAhead * kWarps, page1);          // (the stage read last)
+            if (pages[0] >= 0) unit_of_page<T, FMT, D, NT>(C, ring + (uint32_t)(stage * R::kBytes), u * kUnit + g, u * kUnit + kUnit > sure, lane);
+#pragma unroll
+            for (int i = 0; i + 1 < kAhead; ++i) pages[i] = pages[i + 1];
+            pages[kAhead - 1] = page1;
+            page1 = page2;
+            if (++stage == R::kStages) stage = 0;
+            __syncwarp();
+        }
+        cp_wait<0>();
+        __syncthreads();                                   // the rings give way to the sums
         // ---- join the warps ----
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -602,15 +768,14 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
                 }
             }
         __syncthreads();
-        const bool lone = s0 == 0 && s1 == row.units;
-        const int cta0 = (int)(pair0 / per), n_seg = (int)((pair0 + row.units - 1) / per) - cta0 + 1;
-        float* mine = a.part + ((size_t)2 * blockIdx.x + (s0 == 0 ? 1 : 0)) * kCols * kPitch;
+        const bool lone = n_seg == 1;
+        const int n_col = min(kCols, a.n_q * s.G - ct * kCols);       // columns of the tile that are there
+        float* mine = a.part + ((size_t)2 * blockIdx.x + (line && s0 == 0 ? 1 : 0)) * kCols * kPitch;
         auto store = [&](int col, int e, float4 o, float m, float mp, float l) {
             const int c = ct * kCols + col, qi = c / s.G;
-            if (qi >= a.n_q) return;
             st4(reinterpret_cast<T*>(a.out) + (((size_t)b * a.n_q + qi) * s.Hq + h * s.G + c % s.G) * D + e, finish(o, m, mp, l));
         };
-        for (int i = tid; i < kCols * (D / 4); i += kThreads) {
+        for (int i = tid; i < n_col * (D / 4); i += kThreads) {
             const int col = i / (D / 4), e = (i % (D / 4)) * 4;
             float m = kNegBig, mp = kNegBig, l = 0.f;
 #pragma unroll
@@ -637,28 +802,17 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
                 __threadfence();
             }
             __syncthreads();
-            if (last_s) {
-                for (int i = tid; i < kCols * (D / 4); i += kThreads) {
-                    const int col = i / (D / 4), e = (i % (D / 4)) * 4;
-                    float m = kNegBig, mp = kNegBig, l = 0.f;
-                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int j = 0; j < n_seg; ++j) {      // in the order of the tokens
-                        const float* p = a.part + ((size_t)2 * (cta0 + j) + (j == 0 ? 1 : 0)) * kCols * kPitch + col * kPitch;
-                        const float4 hd = __ldcg(reinterpret_cast<const float4*>(p + D));
-                        const float4 x = __ldcg(reinterpret_cast<const float4*>(p + e));
-                        const float mn = fmaxf(m, hd.x), pn = fmaxf(mp, hd.y);
-                        l = l * pow2_down(m, mn) + hd.z * pow2_down(hd.x, mn);
-                        const float f0 = pow2_down(mp, pn), f1 = pow2_down(hd.y, pn);
-                        o.x = o.x * f0 + x.x * f1; o.y = o.y * f0 + x.y * f1; o.z = o.z * f0 + x.z * f1; o.w = o.w * f0 + x.w * f1;
-                        m = mn;
-                        mp = pn;
-                    }
-                    store(col, e, o, m, mp, l);
-                }
-            }
+            if (last_s) join_parts<T, D, kCols>(a.part, cta0, line, n_seg, n_col, osm, ml, store);
         }
         __syncthreads();
     }
+    // rows without a token: zeros
+    for (int i = blockIdx.x; i < s.B; i += gridDim.x)
+        if (row_plan<STEP>(a, i, false).units == 0) {
+            const int n4 = a.n_q * s.Hq * D / 4;
+            T* o = reinterpret_cast<T*>(a.out) + (size_t)i * a.n_q * s.Hq * D;
+            for (int k = tid; k < n4; k += kThreads) st4(o + (size_t)k * 4, make_float4(0.f, 0.f, 0.f, 0.f));
+        }
     if constexpr (STEP) {                                  // the lengths grow when every CTA is past reading them
         if (tid == 0) {
             last_s = atomicInc(a.tickets + kQ8StepTicket, gridDim.x - 1) == gridDim.x - 1 ? 1 : 0;
@@ -673,6 +827,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
 
 struct Q8Plan {
     int nt, n_ct, ctas;
+    long long units;                 // of all pairs, at most
     size_t smem, part;
 };
 Q8Plan plan_q8(const Q8Dims& s, int n_q, int elt) {
@@ -685,7 +840,12 @@ Q8Plan plan_q8(const Q8Dims& s, int n_q, int elt) {
     const long long most = (long long)sm_count() * (p.nt == 1 && s.d <= 128 && elt == 2 ? 2 : 1), need = (units + kWarps - 1) / kWarps;
     p.ctas = (int)(need < most ? need : most);
     if (p.ctas > kQ8MaxCtas) p.ctas = kQ8MaxCtas;
-    p.smem = (size_t)kWarps * per * (s.d + 4) * sizeof(float);
+    p.units = units;
+    // the rings; the warps' sums; the factors and shares of a join
+    const size_t stage = 32 * (size_t)s.d + 16, rings = kWarps * stage * (elt == 4 && s.d < 256 ? 5 : 3);
+    const size_t warps = (size_t)kWarps * per * (s.d + 4) * sizeof(float), join = (size_t)per * 128 * sizeof(float) + kThreads * 16;
+    p.smem = warps > join ? warps : join;
+    if (rings > p.smem) p.smem = rings;
     p.part = (size_t)2 * p.ctas * per * (s.d + 4) * sizeof(float);
     return p;
 }
@@ -718,6 +878,8 @@ size_t q8_attention_ws_bytes(const Q8Dims& s, int n_q) {
     // the fp32 and the bf16 plan differ in CTAs only
     return 4096 + plan_q8(s, n_q, 2).part;
 }
+
+bool q8_attention_fits(const Q8Dims& s, int n_q) { return plan_q8(s, n_q, 2).units <= 0x7fffffff; }
 
 cudaError_t launch_q8_attention(const Q8Dims& s, const Q8Cache& c, int fmt, int dtype, const void* q, int64_t sb, int64_t si, int64_t sg, void* out, int n_q,
                                 const void* k_new, const void* v_new, char* ws, cudaStream_t stream) {
