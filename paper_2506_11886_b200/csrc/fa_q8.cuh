@@ -9,8 +9,9 @@
 namespace fa {
 
 constexpr int kQ8State = 4;          // int32 words of state per row: tokens, scratch, 2 spare
-constexpr int kQ8MaxCtas = 1000;     // CTAs of an attention launch (tickets in the first 4 KiB of the workspace)
-constexpr int kQ8StepTicket = 1023;  // the ticket that counts the CTAs of a step which have read the lengths
+constexpr int kQ8MaxCtas = 500;      // CTAs of an attention launch; tickets in the first 4 KiB of the workspace: of groups of parts from 0, of
+constexpr int kQ8GroupTickets = 512; // pairs of many groups from here on, and
+constexpr int kQ8StepTicket = 1023;  // of the CTAs of a step which have read the lengths
 
 struct Q8Dims {
     int B, Hq, H, G, d;
@@ -49,6 +50,21 @@ cudaError_t launch_q8_attention(const Q8Dims&, const Q8Cache&, int fmt, int dtyp
                                 const void* k_new, const void* v_new, char* ws, cudaStream_t);
 
 #ifdef __CUDACC__
+// A launch whose CTAs may be scheduled under the tail of the kernel in front (they wait for its end before their first read).
+template <typename... P, typename... A>
+inline cudaError_t launch_behind(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, const A&... args) {
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = grid;
+    c.blockDim = dim3((unsigned)threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = stream;
+    c.attrs = at;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, kernel, args...);
+}
 __device__ __forceinline__ void q8_report(int32_t* status, int err) { atomicCAS(status, (int)FA_OK, err); }
 
 // What a block's values are multiplied by.  A quotient x * top / amax is rounded twice at most (to 32 or 64 bits, then to

@@ -24,8 +24,9 @@
 namespace fa {
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kUnit = 16;            // tokens
+constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kFlat = 40;            // parts that one CTA joins in one go
 
 struct AttnArgs {
     Q8Dims s;
@@ -34,6 +35,7 @@ struct AttnArgs {
     int64_t sb, si, sg;
     void* out;
     int n_q, n_ct;                   // queries a row, column tiles of a KV head
+    int share;                       // CTAs to a (head, column tile) if there is one row, 0 if there are more of these than CTAs
     const void *k_new, *v_new;       // a step
     unsigned* tickets;
     float* part;                     // [2 * CTAs][cols][D + 4]
@@ -423,88 +425,70 @@ __device__ __forceinline__ void push_page(const AttnArgs& a, size_t ph, const T*
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void st4(T* p, float4 v) {
-    if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4*>(p) = v;
-    } else {
-        const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
-        uint2 u;
-        u.x = *reinterpret_cast<const uint32_t*>(&a);
-        u.y = *reinterpret_cast<const uint32_t*>(&b);
-        *reinterpret_cast<uint2*>(p) = u;
-    }
-}
 // o 2^(m' - m - 15) / l, the power of two in two factors; a column that saw nothing is zero.
-__device__ __forceinline__ float4 finish(float4 o, float m, float mp, float l) {
+__device__ __forceinline__ float2 finish(float2 o, float m, float mp, float l) {
     const int e = (int)fminf(fmaxf(mp - m - 15.f, -250.f), 250.f), e0 = e / 2;
     const float f = pow2i(e0), f2 = pow2i(e - e0), r = l == 0.f ? 0.f : 1.f / l;
-    return make_float4(o.x * r * f * f2, o.y * r * f * f2, o.z * r * f * f2, o.w * r * f * f2);
+    return make_float2(o.x * r * f * f2, o.y * r * f * f2);
 }
 
-// The parts of one pair, in the order of the tokens: a warp per column finds the maxima and every part's factor, then each
-// thread sums four dims of a column over its share of the parts (a few shares where the columns are few), with loads of
-// eight parts in flight.
-template <typename T, int D, int kCols, typename Store>
-__device__ __forceinline__ void join_parts(const float* part, int cta0, bool line, int n_seg, int n_col, float* sm, float (&ml)[3][kWarps][kCols], const Store& store) {
-    constexpr int kPitch = D + 4, kChunk = 128;            // parts whose factors lie in shared memory at a time: [column][kChunk]
+// The n <= kFlat parts at p, p + step, ... of a pair to one, in that order: sums go to out(column, dim, two sums, m, m', l).  The first
+// loads are in flight while a warp for each column finds the maxima and the parts' factors.  (Code that runs once costs by its length, its
+// instructions come from L2: few of them, in loops.)
+template <int D, int kCols, typename Out>
+__device__ __forceinline__ void join_parts(const float* p, size_t step, int n, int n_col, float* fac, float (*ml)[kWarps][kCols], const Out& out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    auto at = [&](int j, int col) { return part + ((size_t)2 * (cta0 + j) + (line && j == 0 ? 1 : 0)) * kCols * kPitch + col * kPitch; };
-    for (int col = warp; col < n_col; col += kWarps) {
-        float m = kNegBig, mp = kNegBig, l = 0.f;
-        for (int j = lane; j < n_seg; j += 32) {
-            const float4 hd = __ldcg(reinterpret_cast<const float4*>(at(j, col) + D));
-            const float mn = fmaxf(m, hd.x);
-            l = l * pow2_down(m, mn) + hd.z * pow2_down(hd.x, mn);
-            m = mn;
-            mp = fmaxf(mp, hd.y);
-        }
-        const float mx = warp_max(m);
-        mp = warp_max(mp);
-        l = warp_sum(l * pow2_down(m, mx));
-        if (lane == 0) { ml[0][0][col] = mx; ml[1][0][col] = mp; ml[2][0][col] = l; }
-    }
-    const int slots = n_col * (D / 4), shares = slots <= kThreads / 2 ? kThreads / slots : 1;
-    float* fac = sm;                                       // [kCols][kChunk]
-    float4* acc = reinterpret_cast<float4*>(sm + kCols * kChunk);      // [shares - 1][slots]
-    for (int i0 = 0; i0 < slots; i0 += kThreads) {
-        const int i = shares > 1 ? tid % slots : i0 + tid, share = shares > 1 ? tid / slots : 0;
-        const bool on = i < slots && share < shares;
-        const int col = i / (D / 4), e = (i % (D / 4)) * 4;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int j0 = 0; j0 < n_seg; j0 += kChunk) {
-            const int n = min(kChunk, n_seg - j0);
-            __syncthreads();
-            for (int k = tid; k < n_col * kChunk; k += kThreads) {
-                const int c = k / kChunk, j = k % kChunk;
-                if (j < n) fac[k] = pow2_down(__ldcg(at(j0 + j, c) + D + 1), ml[1][0][c]);
-            }
-            __syncthreads();
-            if (!on) continue;
-            for (int j = share; j < n; j += 8 * shares) {
-                float4 x[8];
+    constexpr int kFly = 20, kPitch = D + 4;
+    float2 x[kFly];
+#pragma unroll 1
+    for (int i0 = 0; i0 < n_col * (D / 2); i0 += kThreads) {
+        const int i = i0 + tid, col = min(i / (D / 2), n_col - 1), e = i % (D / 2) * 2;
+        float2 o = make_float2(0.f, 0.f);
+#pragma unroll 1
+        for (int k0 = 0; k0 < n; k0 += kFly) {
+            const float* q = p + step * k0 + col * kPitch + e;
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (j + k * shares < n) x[k] = __ldcg(reinterpret_cast<const float4*>(at(j0 + j + k * shares, col) + e));
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (j + k * shares < n) {
-                        const float f = fac[col * kChunk + j + k * shares];
-                        o.x = fmaf(x[k].x, f, o.x); o.y = fmaf(x[k].y, f, o.y); o.z = fmaf(x[k].z, f, o.z); o.w = fmaf(x[k].w, f, o.w);
-                    }
+            for (int k = 0; k < kFly; ++k) {
+                if (k0 + k < n) x[k] = __ldcg(reinterpret_cast<const float2*>(q));
+                else x[k] = make_float2(0.f, 0.f);
+                q += step;
             }
-        }
-        if (shares > 1) {
-            if (on && share > 0) acc[(share - 1) * slots + i] = o;
-            __syncthreads();
-            if (share == 0)
-                for (int k = 1; k < shares; ++k) {
-                    const float4 x = acc[(k - 1) * slots + i];
-                    o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+            if (i0 == 0 && k0 == 0) {
+#pragma unroll 1
+                for (int c = warp; c < n_col; c += kWarps) {
+                    static_assert(kFlat <= 64, "two parts to a lane");
+                    const float4 none = make_float4(kNegBig, kNegBig, 0.f, 0.f);
+                    const float* hd = p + step * lane + c * kPitch + D;
+                    const float4 u = lane < n ? __ldcg(reinterpret_cast<const float4*>(hd)) : none;
+                    const float4 v = lane + 32 < n ? __ldcg(reinterpret_cast<const float4*>(hd + 32 * step)) : none;
+                    const float m = warp_max(fmaxf(u.x, v.x)), mp = warp_max(fmaxf(u.y, v.y));
+                    const float l = warp_sum(fmaf(u.z, pow2_down(u.x, m), v.z * pow2_down(v.x, m)));
+                    fac[c * 64 + lane] = pow2_down(u.y, mp);
+                    fac[c * 64 + lane + 32] = pow2_down(v.y, mp);
+                    if (lane == 0) { ml[0][0][c] = m; ml[1][0][c] = mp; ml[2][0][c] = l; }
                 }
+                __syncthreads();
+            }
+#pragma unroll
+            for (int k = 0; k < kFly; ++k) {
+                const float f = fac[col * 64 + min(k0 + k, 63)];
+                o.x = fmaf(x[k].x, f, o.x);
+                o.y = fmaf(x[k].y, f, o.y);
+            }
         }
-        if (on && share == 0) store(col, e, o, ml[0][0][col], ml[1][0][col], ml[2][0][col]);
+        if (i < n_col * (D / 2)) out(col, e, o, ml[0][0][col], ml[1][0][col], ml[2][0][col]);
     }
+}
+// One arrival of the CTA, whose writes are done, on a ticket of n; true for the last one, which sees the others' writes.
+__device__ __forceinline__ bool arrive_last(unsigned* ticket, int n, int* flag) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        *flag = atomicInc(ticket, (unsigned)(n - 1)) == (unsigned)(n - 1) ? 1 : 0;
+        __threadfence();
+    }
+    __syncthreads();
+    return *flag != 0;
 }
 
 template <typename T, int FMT, int D, int NT, bool STEP>
@@ -514,13 +498,15 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
     using R = Ring<T, D>;
     extern __shared__ float4 smem4[];
     float* osm = reinterpret_cast<float*>(smem4);          // the rings; then [warps][columns][pitch]; then a join's factors and shares
-    __shared__ float ml[3][kWarps][kCols];
+    __shared__ float ml[3][kWarps][kCols], wf[kCols][kWarps];
     __shared__ int last_s;
     const Q8Dims& s = a.s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const unsigned per_row = (unsigned)(s.H * a.n_ct), ctas = gridDim.x;
     const uint32_t ring = smem_addr(smem4) + (uint32_t)(warp * R::kStages * R::kBytes);
 
+    asm volatile("griddepcontrol.launch_dependents;");       // the next call's CTAs may come; this one's wait for what is in front of it
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     // ---- this CTA's part, found by every warp for itself; lanes hold 32 rows at a time ----
     RowPlan mine = {0, 0, 0, false};
     auto rows_from = [&](int b0, bool tell) {              // (up to 32 rows are loaded once)
@@ -528,59 +514,70 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
         mine = RowPlan{0, 0, 0, false};
         if (b0 + lane < s.B) mine = row_plan<STEP>(a, b0 + lane, tell && blockIdx.x == 0 && warp == 0);
     };
-    unsigned total = 0, pairs = 0, most = 0;
-    for (int b0 = 0; b0 < s.B; b0 += 32) {
-        rows_from(b0, true);
-        total += __reduce_add_sync(0xffffffffu, (unsigned)mine.units * per_row);
-        pairs += (unsigned)__popc(__ballot_sync(0xffffffffu, mine.units > 0)) * per_row;
-        most = max(most, __reduce_max_sync(0xffffffffu, (unsigned)mine.units));
-    }
-    // Fewer pairs than CTAs: the smallest parts (of 8 units at least, one for each warp) that are no more than the CTAs.
-    // Each lane tries a size, 2^(1/10) apart from total / CTAs on, the last one that of the longest pair.
-    const bool line = pairs > ctas;
-    unsigned per = max((total + ctas - 1) / ctas, (unsigned)kWarps);
-    if (!line) {
-        const unsigned size = lane == 31 ? max(most, per) : (unsigned)ceilf((float)per * exp2f(0.1f * (float)lane));
-        unsigned parts = 0;
-        for (int b0 = 0; b0 < s.B; b0 += 32) {
-            rows_from(b0, false);
-            for (int i = 0; i < min(32, s.B - b0); ++i) parts += ((unsigned)__shfl_sync(0xffffffffu, mine.units, i) + size - 1) / size * per_row;
-        }
-        per = __shfl_sync(0xffffffffu, size, __ffs(__ballot_sync(0xffffffffu, parts <= ctas)) - 1);
-    }
-    unsigned u0 = line ? min(per * blockIdx.x, total) : blockIdx.x;  // in units of the line, or in parts
-    const unsigned u1 = line ? min(u0 + per, total) : blockIdx.x + 1;
+    bool line = false;
+    unsigned per = kWarps, u0 = blockIdx.x, u1 = blockIdx.x + 1;     // units of a part; this CTA's: of the line, or the number of its part
     unsigned base = 0;                                               // units (parts) in front of row b
     int b = 0;
     RowPlan row = {0, 0, 0, false};
     auto of_row = [&](int units) { return (line ? (unsigned)units : ((unsigned)units + per - 1) / per) * per_row; };
-    {
-        bool found = false;
-        unsigned before = 0;
-        for (int b0 = 0; b0 < s.B && !found; b0 += 32) {
-            rows_from(b0, false);
-            const unsigned n = of_row(mine.units);
-            unsigned v = n;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const unsigned w = __shfl_up_sync(0xffffffffu, v, d);
-                if (lane >= d) v += w;
-            }
-            const unsigned hit = __ballot_sync(0xffffffffu, before + v > u0);
-            if (hit) {
-                const int src = __ffs(hit) - 1;
-                b = b0 + src;
-                base = before + __shfl_sync(0xffffffffu, v - n, src);
-                row.len = __shfl_sync(0xffffffffu, mine.len, src);
-                row.first = __shfl_sync(0xffffffffu, mine.first, src);
-                row.units = __shfl_sync(0xffffffffu, mine.units, src);
-                row.push = __shfl_sync(0xffffffffu, (int)mine.push, src);
-                found = true;
-            }
-            before += __shfl_sync(0xffffffffu, v, 31);
-        }
-        if (!found) u0 = u1;                               // nothing left for this CTA
+    if (s.B == 1) {                                                  // (a.share: CTAs to a pair)
+        row = row_plan<STEP>(a, 0, blockIdx.x == 0 && tid == 0);
+        if (a.share > 0) per = max(((unsigned)row.units + a.share - 1) / (unsigned)a.share, (unsigned)kWarps);
     }
+    if (s.B > 1 || a.share == 0) {
+        unsigned total = 0, pairs = 0, most = 0;
+        for (int b0 = 0; b0 < s.B; b0 += 32) {
+            rows_from(b0, true);
+            total += __reduce_add_sync(0xffffffffu, (unsigned)mine.units * per_row);
+            pairs += (unsigned)__popc(__ballot_sync(0xffffffffu, mine.units > 0)) * per_row;
+            most = max(most, __reduce_max_sync(0xffffffffu, (unsigned)mine.units));
+        }
+        // Fewer pairs than CTAs: the smallest parts (of a unit for each warp at least) that are no more than the CTAs.
+        // Each lane tries a size, 2^(1/10) apart from total / CTAs on, the last one that of the longest pair.
+        line = pairs > ctas;
+        per = max((total + ctas - 1) / ctas, (unsigned)kWarps);
+        if (!line) {
+            const unsigned size = lane == 31 ? max(most, per) : (unsigned)ceilf((float)per * exp2f(0.1f * (float)lane));
+            unsigned parts = 0;
+            for (int b0 = 0; b0 < s.B; b0 += 32) {
+                rows_from(b0, false);
+                for (int i = 0; i < min(32, s.B - b0); ++i) parts += ((unsigned)__shfl_sync(0xffffffffu, mine.units, i) + size - 1) / size * per_row;
+            }
+            per = __shfl_sync(0xffffffffu, size, __ffs(__ballot_sync(0xffffffffu, parts <= ctas)) - 1);
+        }
+        if (line) {
+            u0 = min(per * blockIdx.x, total);
+            u1 = min(u0 + per, total);
+        }
+        {
+            bool found = false;
+            unsigned before = 0;
+            for (int b0 = 0; b0 < s.B && !found; b0 += 32) {
+                rows_from(b0, false);
+                const unsigned n = of_row(mine.units);
+                unsigned v = n;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const unsigned w = __shfl_up_sync(0xffffffffu, v, d);
+                    if (lane >= d) v += w;
+                }
+                const unsigned hit = __ballot_sync(0xffffffffu, before + v > u0);
+                if (hit) {
+                    const int src = __ffs(hit) - 1;
+                    b = b0 + src;
+                    base = before + __shfl_sync(0xffffffffu, v - n, src);
+                    row.len = __shfl_sync(0xffffffffu, mine.len, src);
+                    row.first = __shfl_sync(0xffffffffu, mine.first, src);
+                    row.units = __shfl_sync(0xffffffffu, mine.units, src);
+                    row.push = __shfl_sync(0xffffffffu, (int)mine.push, src);
+                    found = true;
+                }
+                before += __shfl_sync(0xffffffffu, v, 31);
+            }
+            if (!found) u0 = u1;
+        }
+    }
+    if (u0 >= u1 || (s.B == 1 && u0 >= of_row(row.units))) u0 = u1;      // nothing left for this CTA
 
     while (u0 < u1) {
         if (u0 >= base + of_row(row.units)) {              // (a line only)
@@ -616,7 +613,18 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
         const int sure = row.len - a.n_q + 1 + ct * kCols / s.G;                                 // ... that all columns see
         const int stop = min(min(s1, paged), (seen + kUnit - 1) / kUnit);
 
-        // ---- loads: the tail's unit, the first unit in pages ----
+        // ---- loads: q, the tail's unit, the first unit in pages ----
+        Vec16<T> qv[NT][D / 64];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int col = ct * kCols + nt * 8 + g, qi = s.G == 1 ? col : col / s.G, gq = col - qi * s.G;
+            const T* qp = reinterpret_cast<const T*>(a.q) + (int64_t)b * a.sb + (int64_t)qi * a.si + (int64_t)(h * s.G + gq) * a.sg;
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+                if (qi < a.n_q) qv[nt][c].load(qp + k_dim<D>(c, t));
+                else qv[nt][c].zero();
+            }
+        }
         auto page_of = [&](int u) {
             if (u >= stop) return -1;
             const int p = table[u >> lu];
@@ -673,17 +681,10 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
         Columns<T, D, NT> C;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int col = ct * kCols + nt * 8 + g, qi = col / s.G, gq = col % s.G;
-            const bool there = qi < a.n_q;
-            const T* qp = reinterpret_cast<const T*>(a.q) + (int64_t)b * a.sb + (int64_t)qi * a.si + (int64_t)(h * s.G + gq) * a.sg;
-            Vec16<T> v[D / 64];
+            const int qi = (ct * kCols + nt * 8 + g) / s.G;
             uint32_t mxq = 0;
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) {
-                if (there) v[c].load(qp + k_dim<D>(c, t));
-                else v[c].zero();
-                mxq = max(mxq, v[c].amax_bits());
-            }
+            for (int c = 0; c < D / 64; ++c) mxq = max(mxq, qv[nt][c].amax_bits());
             mxq = max(mxq, __shfl_xor_sync(0xffffffffu, mxq, 1));
             mxq = max(mxq, __shfl_xor_sync(0xffffffffu, mxq, 2));
             const int e = max((int)(mxq >> 23) - 127, -100);            // (an infinity or NaN stays one in the product)
@@ -694,11 +695,11 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        C.q[nt][4 * c + j][k] = pair_of(v[c], 4 * j + 2 * k, f, false);
-                        if constexpr (kF32) C.ql[nt][4 * c + j][k] = pair_of(v[c], 4 * j + 2 * k, f, true);
+                        C.q[nt][4 * c + j][k] = pair_of(qv[nt][c], 4 * j + 2 * k, f, false);
+                        if constexpr (kF32) C.ql[nt][4 * c + j][k] = pair_of(qv[nt][c], 4 * j + 2 * k, f, true);
                     }
             const float fcol = pow2i(e - 13) * (s.scale * kLog2e);
-            const int lastq = there ? row.len - a.n_q + qi : -1;
+            const int lastq = qi < a.n_q ? row.len - a.n_q + qi : -1;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 C.f[nt][k] = __shfl_sync(0xffffffffu, fcol, (2 * t + k) * 4);
@@ -738,88 +739,98 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
         cp_wait<0>();
         __syncthreads();                                   // the rings give way to the sums
         // ---- join the warps ----
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                for (int d = 4; d < 32; d <<= 1) C.l[nt][k] += __shfl_xor_sync(0xffffffffu, C.l[nt][k], d);
-                if (g == 0) {
-                    ml[0][warp][nt * 8 + 2 * t + k] = C.m[nt][k];
-                    ml[1][warp][nt * 8 + 2 * t + k] = C.mp[nt][k];
-                    ml[2][warp][nt * 8 + 2 * t + k] = C.l[nt][k];
-                }
-            }
-        __syncthreads();
+        const int n_col = min(kCols, a.n_q * s.G - ct * kCols);      // columns of the tile that are there
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int col = nt * 8 + 2 * t + k;
-                float mp = kNegBig;
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) mp = fmaxf(mp, ml[1][w][col]);
-                const float f = pow2_down(C.mp[nt][k], mp);
-                float* dst = osm + ((size_t)warp * kCols + col) * kPitch;
+                for (int d = 4; d < 32; d <<= 1) C.l[nt][k] += __shfl_xor_sync(0xffffffffu, C.l[nt][k], d);
+                if (g == 0) { ml[0][warp][col] = C.m[nt][k]; ml[1][warp][col] = C.mp[nt][k]; ml[2][warp][col] = C.l[nt][k]; }
+                if (col < n_col) {
+                    float* dst = osm + ((size_t)warp * kCols + col) * kPitch;
 #pragma unroll
-                for (int i = 0; i < kMt; ++i) {
-                    const int d = D == 64 ? 8 * g + 2 * i : 128 * (i >> 3) + 16 * g + 2 * (i & 7);
-                    *reinterpret_cast<float2*>(dst + d) = make_float2(C.o[nt][i][k] * f, C.o[nt][i][2 + k] * f);
+                    for (int i = 0; i < kMt; ++i) {
+                        const int d = D == 64 ? 8 * g + 2 * i : 128 * (i >> 3) + 16 * g + 2 * (i & 7);
+                        *reinterpret_cast<float2*>(dst + d) = make_float2(C.o[nt][i][k], C.o[nt][i][2 + k]);
+                    }
                 }
             }
         __syncthreads();
-        const bool lone = n_seg == 1;
-        const int n_col = min(kCols, a.n_q * s.G - ct * kCols);       // columns of the tile that are there
-        float* mine = a.part + ((size_t)2 * blockIdx.x + (line && s0 == 0 ? 1 : 0)) * kCols * kPitch;
-        auto store = [&](int col, int e, float4 o, float m, float mp, float l) {
+        auto store = [&](int col, int e, float2 o, float m, float mp, float l) {
             const int c = ct * kCols + col, qi = c / s.G;
-            st4(reinterpret_cast<T*>(a.out) + (((size_t)b * a.n_q + qi) * s.Hq + h * s.G + c % s.G) * D + e, finish(o, m, mp, l));
+            T* p = reinterpret_cast<T*>(a.out) + (((size_t)b * a.n_q + qi) * s.Hq + h * s.G + c - qi * s.G) * D + e;
+            const float2 r = finish(o, m, mp, l);
+            if constexpr (kF32) *reinterpret_cast<float2*>(p) = r;
+            else *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(r.x, r.y);
         };
-        for (int i = tid; i < n_col * (D / 4); i += kThreads) {
-            const int col = i / (D / 4), e = (i % (D / 4)) * 4;
-            float m = kNegBig, mp = kNegBig, l = 0.f;
+        // Parts of a pair lie one behind the other from 2 x its first CTA + 1 on: in a line a CTA can be the last of one pair and the first
+        // of the next (those in between have no other part), and the next pair's places then start past this one's.
+        constexpr size_t kPart = (size_t)kCols * kPitch;
+        float* parts = a.part + (size_t)(2 * cta0 + 1) * kPart;
+        auto keep = [&](int j) {
+            return [=](int col, int e, float2 o, float m, float mp, float l) {
+                float* p = parts + (size_t)j * kPart + col * kPitch;
+                *reinterpret_cast<float2*>(p + e) = o;
+                if (e == 0) *reinterpret_cast<float4*>(p + D) = make_float4(m, mp, l, 0.f);
+            };
+        };
+        const int mine_j = (int)blockIdx.x - cta0;                   // this part's place in the pair
+        const auto keep_mine = keep(mine_j);
+        if (tid < n_col * kWarps) {                                  // the warps' factors, in the places of their maxima
+            const int col = tid / kWarps, w = tid % kWarps;
+            float m = ml[0][w][col], mp = ml[1][w][col], l = ml[2][w][col];
+            const unsigned group = 0xffu << (lane & 24);
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) { m = fmaxf(m, ml[0][w][col]); mp = fmaxf(mp, ml[1][w][col]); }
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int d = 1; d < kWarps; d <<= 1) { m = fmaxf(m, __shfl_xor_sync(group, m, d)); mp = fmaxf(mp, __shfl_xor_sync(group, mp, d)); }
+            l *= pow2_down(ml[0][w][col], m);
+#pragma unroll
+            for (int d = 1; d < kWarps; d <<= 1) l += __shfl_xor_sync(group, l, d);
+            wf[col][w] = pow2_down(ml[1][w][col], mp);
+            if (w == 0) { ml[0][0][col] = m; ml[1][0][col] = mp; ml[2][0][col] = l; }
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int i = tid; i < n_col * (D / 2); i += kThreads) {
+            const int col = i / (D / 2), e = i % (D / 2) * 2;
+            float2 o = make_float2(0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                l += ml[2][w][col] * pow2_down(ml[0][w][col], m);
-                const float4 x = *reinterpret_cast<const float4*>(osm + ((size_t)w * kCols + col) * kPitch + e);
-                o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+                const float2 x = *reinterpret_cast<const float2*>(osm + ((size_t)w * kCols + col) * kPitch + e);
+                o.x = fmaf(x.x, wf[col][w], o.x);
+                o.y = fmaf(x.y, wf[col][w], o.y);
             }
-            if (lone) {
-                store(col, e, o, m, mp, l);
-            } else {
-                *reinterpret_cast<float4*>(mine + col * kPitch + e) = o;
-                if (e == 0) *reinterpret_cast<float4*>(mine + col * kPitch + D) = make_float4(m, mp, l, 0.f);
-            }
+            if (n_seg == 1) store(col, e, o, ml[0][0][col], ml[1][0][col], ml[2][0][col]);
+            else keep_mine(col, e, o, ml[0][0][col], ml[1][0][col], ml[2][0][col]);
         }
-        if (!lone) {
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                last_s = atomicInc(a.tickets + cta0, n_seg - 1) == (unsigned)(n_seg - 1) ? 1 : 0;
-                __threadfence();
+        // ---- join the parts; many of them by groups, each by its last part to finish, then the groups by the last of those ----
+        if (n_seg > 1) {
+            int size = n_seg;
+            if (n_seg > kFlat) {
+                size = 7;
+                while (size * size < n_seg) ++size;                  // (n_seg <= 500: 23 at most)
+                const int j0 = mine_j / size * size, n = min(size, n_seg - j0);
+                if (n == 1 || arrive_last(a.tickets + cta0 + j0, n, &last_s)) {
+                    if (n > 1) join_parts<D, kCols>(parts + j0 * kPart, kPart, n, n_col, osm, ml, keep(j0));
+                    if (arrive_last(a.tickets + kQ8GroupTickets + cta0, (n_seg + size - 1) / size, &last_s))
+                        join_parts<D, kCols>(parts, size * kPart, (n_seg + size - 1) / size, n_col, osm, ml, store);
+                }
+            } else if (arrive_last(a.tickets + cta0, n_seg, &last_s)) {
+                join_parts<D, kCols>(parts, kPart, n_seg, n_col, osm, ml, store);
             }
-            __syncthreads();
-            if (last_s) join_parts<T, D, kCols>(a.part, cta0, line, n_seg, n_col, osm, ml, store);
         }
         __syncthreads();
     }
     // rows without a token: zeros
     for (int i = blockIdx.x; i < s.B; i += gridDim.x)
         if (row_plan<STEP>(a, i, false).units == 0) {
-            const int n4 = a.n_q * s.Hq * D / 4;
-            T* o = reinterpret_cast<T*>(a.out) + (size_t)i * a.n_q * s.Hq * D;
-            for (int k = tid; k < n4; k += kThreads) st4(o + (size_t)k * 4, make_float4(0.f, 0.f, 0.f, 0.f));
+            const size_t n16 = (size_t)a.n_q * s.Hq * D * sizeof(T) / 16;
+            uint4* o = reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.out) + (size_t)i * a.n_q * s.Hq * D);
+            for (size_t k = tid; k < n16; k += kThreads) o[k] = make_uint4(0u, 0u, 0u, 0u);
         }
     if constexpr (STEP) {                                  // the lengths grow when every CTA is past reading them
-        if (tid == 0) {
-            last_s = atomicInc(a.tickets + kQ8StepTicket, gridDim.x - 1) == gridDim.x - 1 ? 1 : 0;
-            __threadfence();
-        }
-        __syncthreads();
-        if (last_s)
+        if (arrive_last(a.tickets + kQ8StepTicket, (int)gridDim.x, &last_s))
             for (int i = tid; i < s.B; i += kThreads)
                 if (row_plan<true>(a, i, false).push) a.c.state[i * kQ8State] += 1;
     }
@@ -836,32 +847,26 @@ Q8Plan plan_q8(const Q8Dims& s, int n_q, int elt) {
     p.nt = cols <= 8 ? 1 : 2;
     const int per = 8 * p.nt;
     p.n_ct = (int)((cols + per - 1) / per);
-    const long long units = (long long)s.B * s.H * p.n_ct * ((long long)s.nb * s.blk / kUnit + 1);
-    const long long most = (long long)sm_count() * (p.nt == 1 && s.d <= 128 && elt == 2 ? 2 : 1), need = (units + kWarps - 1) / kWarps;
+    p.units = (long long)s.B * s.H * p.n_ct * ((long long)s.nb * s.blk / kUnit + 1);
+    const long long most = (long long)sm_count() * (p.nt == 1 && s.d <= 128 && elt == 2 ? 2 : 1);
+    const long long pairs = (long long)s.B * s.H * p.n_ct, parts = (p.units + kWarps - 1) / kWarps, need = parts > pairs ? parts : pairs;
     p.ctas = (int)(need < most ? need : most);
     if (p.ctas > kQ8MaxCtas) p.ctas = kQ8MaxCtas;
-    p.units = units;
-    // the rings; the warps' sums; the factors and shares of a join
+    // the rings; the warps' sums; the factors of the parts that are joined
     const size_t stage = 32 * (size_t)s.d + 16, rings = kWarps * stage * (elt == 4 && s.d < 256 ? 5 : 3);
-    const size_t warps = (size_t)kWarps * per * (s.d + 4) * sizeof(float), join = (size_t)per * 128 * sizeof(float) + kThreads * 16;
-    p.smem = warps > join ? warps : join;
-    if (rings > p.smem) p.smem = rings;
+    const size_t sums = (size_t)kWarps * per * (s.d + 4) * sizeof(float), heads = 64 * (size_t)per * sizeof(float);
+    p.smem = rings > sums ? rings : sums;
+    if (heads > p.smem) p.smem = heads;
     p.part = (size_t)2 * p.ctas * per * (s.d + 4) * sizeof(float);
     return p;
 }
 
 template <typename T, int FMT, int D, int NT>
 cudaError_t attn_of(const AttnArgs& a, const Q8Plan& p, cudaStream_t stream) {
-    if (a.k_new) {
-        cudaError_t e = ensure_dynamic_smem(q8_attn_kernel<T, FMT, D, NT, true>, p.smem);
-        if (e != cudaSuccess) return e;
-        q8_attn_kernel<T, FMT, D, NT, true><<<p.ctas, kThreads, p.smem, stream>>>(a);
-    } else {
-        cudaError_t e = ensure_dynamic_smem(q8_attn_kernel<T, FMT, D, NT, false>, p.smem);
-        if (e != cudaSuccess) return e;
-        q8_attn_kernel<T, FMT, D, NT, false><<<p.ctas, kThreads, p.smem, stream>>>(a);
-    }
-    return cudaGetLastError();
+    const auto kernel = a.k_new ? q8_attn_kernel<T, FMT, D, NT, true> : q8_attn_kernel<T, FMT, D, NT, false>;
+    const cudaError_t e = ensure_dynamic_smem(kernel, p.smem);
+    if (e != cudaSuccess) return e;
+    return launch_behind(kernel, dim3((unsigned)p.ctas), kThreads, p.smem, stream, a);
 }
 template <typename T, int FMT>
 cudaError_t attn_dims(const AttnArgs& a, const Q8Plan& p, cudaStream_t stream) {
@@ -875,8 +880,8 @@ cudaError_t attn_dims(const AttnArgs& a, const Q8Plan& p, cudaStream_t stream) {
 }  // namespace
 
 size_t q8_attention_ws_bytes(const Q8Dims& s, int n_q) {
-    // the fp32 and the bf16 plan differ in CTAs only
-    return 4096 + plan_q8(s, n_q, 2).part;
+    const size_t a = plan_q8(s, n_q, 2).part, b = plan_q8(s, n_q, 4).part;
+    return 4096 + (a > b ? a : b);
 }
 
 bool q8_attention_fits(const Q8Dims& s, int n_q) { return plan_q8(s, n_q, 2).units <= 0x7fffffff; }
@@ -884,7 +889,7 @@ bool q8_attention_fits(const Q8Dims& s, int n_q) { return plan_q8(s, n_q, 2).uni
 cudaError_t launch_q8_attention(const Q8Dims& s, const Q8Cache& c, int fmt, int dtype, const void* q, int64_t sb, int64_t si, int64_t sg, void* out, int n_q,
                                 const void* k_new, const void* v_new, char* ws, cudaStream_t stream) {
     const Q8Plan p = plan_q8(s, n_q, dtype == FA_BF16 ? 2 : 4);
-    const AttnArgs a = {s, c, q, sb, si, sg, out, n_q, p.n_ct, k_new, v_new, reinterpret_cast<unsigned*>(ws), reinterpret_cast<float*>(ws + 4096)};
+    const AttnArgs a = {s, c, q, sb, si, sg, out, n_q, p.n_ct, (int)(p.ctas / ((long long)s.H * p.n_ct)), k_new, v_new, reinterpret_cast<unsigned*>(ws), reinterpret_cast<float*>(ws + 4096)};
     if (dtype == FA_BF16) return fmt == FA_Q8_INT8 ? attn_dims<__nv_bfloat16, FA_Q8_INT8>(a, p, stream) : attn_dims<__nv_bfloat16, FA_Q8_E4M3>(a, p, stream);
     return fmt == FA_Q8_INT8 ? attn_dims<float, FA_Q8_INT8>(a, p, stream) : attn_dims<float, FA_Q8_E4M3>(a, p, stream);
 }
