@@ -880,14 +880,15 @@ cudaError_t attn_dims(const AttnArgs& a, const Q8Plan& p, cudaStream_t stream) {
 }  // namespace
 
 size_t q8_attention_ws_bytes(const Q8Dims& s, int n_q) {
-    const size_t a = plan_q8(s, n_q, 2).part, b = plan_q8(s, n_q, 4).part;
-    return 4096 + (a > b ? a : b);
+    const size_t a = 4096 + plan_q8(s, n_q, 2).part, b = 4096 + plan_q8(s, n_q, 4).part, c = q8_chunk_takes(s, FA_BF16, n_q) ? q8_chunk_ws_bytes(s) : 0;
+    return a > b ? (a > c ? a : c) : (b > c ? b : c);
 }
 
 bool q8_attention_fits(const Q8Dims& s, int n_q) { return plan_q8(s, n_q, 2).units <= 0x7fffffff; }
 
 cudaError_t launch_q8_attention(const Q8Dims& s, const Q8Cache& c, int fmt, int dtype, const void* q, int64_t sb, int64_t si, int64_t sg, void* out, int n_q,
                                 const void* k_new, const void* v_new, char* ws, cudaStream_t stream) {
+    if (!k_new && q8_chunk_takes(s, dtype, n_q)) return launch_q8_chunk(s, c, fmt, q, sb, si, sg, out, n_q, ws, stream);
     const Q8Plan p = plan_q8(s, n_q, dtype == FA_BF16 ? 2 : 4);
     const AttnArgs a = {s, c, q, sb, si, sg, out, n_q, p.n_ct, (int)(p.ctas / ((long long)s.H * p.n_ct)), k_new, v_new, reinterpret_cast<unsigned*>(ws), reinterpret_cast<float*>(ws + 4096)};
     if (dtype == FA_BF16) return fmt == FA_Q8_INT8 ? attn_dims<__nv_bfloat16, FA_Q8_INT8>(a, p, stream) : attn_dims<__nv_bfloat16, FA_Q8_E4M3>(a, p, stream);

@@ -280,6 +280,39 @@ def test_attention_matches_its_definition(fmt, dtype, Hq, H, d, block, n_q):
 
 
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("Hq,H,d,block,n_q", [(8, 2, 128, 64, 100), (4, 1, 64, 16, 16), (3, 3, 64, 128, 257), (12, 4, 128, 16, 200), (16, 1, 128, 128, 33), (4, 2, 128, 32, 640)])
+def test_chunks_of_queries_match_their_definition(fmt, Hq, H, d, block, n_q):
+    """Rows shorter than the chunk, empty, around a tile of 128 tokens and a block, cut into several parts; tiles of queries that are not full."""
+    lens = [0, 1, 17, 127, 128, 129, n_q, n_q + 1, 5 * block + 3, 1000]
+    B, most = len(lens), 1024
+    lay, cache = make(B=B, Hq=Hq, H=H, d=d, block=block, nb=most // block, fmt=fmt)
+    K, V = rand((B, most, H, d), "bf16", 1), rand((B, most, H, d), "bf16", 2)
+    fa.fa_q8_write(lay, cache, K, V, torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    rows = ref.Rows(B, H, d, block, fmt, torch.bfloat16)
+    for b in range(B):
+        rows.push(b, K[b, :lens[b]], V[b, :lens[b]])
+    q = rand((B, n_q, Hq, d), "bf16", 3)
+    out, _ = attend_and_check(lay, cache, rows, q, "bf16")
+    assert (out[0] == 0).all()
+    wide = torch.full((B, n_q, Hq + 3, d), float("nan"), dtype=q.dtype, device="cuda")
+    wide[:, :, 1:1 + Hq] = q
+    again, _ = attend_and_check(lay, cache, rows, q, "bf16", view=wide[:, :, 1:1 + Hq])
+    assert torch.equal(out, again)
+
+
+def test_a_long_row_and_one_tile_of_queries():
+    """One tile of queries over 30 000 tokens, cut into as many parts as there are SMs; blocks of very different scales."""
+    Hq, H, d, block, n = 4, 1, 128, 64, 30000
+    lay, cache = make(Hq=Hq, H=H, d=d, block=block, nb=470)
+    K, V = rand((1, n, H, d), "bf16", 1), rand((1, n, H, d), "bf16", 2)
+    V = (V.float() * 10.0 ** (torch.arange(n, device="cuda") // 700 % 13 - 6)[None, :, None, None]).bfloat16()
+    fa.fa_q8_write(lay, cache, K, V)
+    rows = ref.Rows(1, H, d, block, "int8", torch.bfloat16)
+    rows.push(0, K[0], V[0])
+    attend_and_check(lay, cache, rows, rand((1, 40, Hq, d), "bf16", 3), "bf16")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 def test_long_rows_and_many_parts(fmt):
     """A row of 20 001 tokens in many parts beside a short one; nearly equal and very different scores."""
     B, Hq, H, d, block = 2, 8, 2, 128, 64
