@@ -6,11 +6,12 @@
 // tensor memory.  The two tiles take turns: the tensor cores work for one while the other's weights are formed.
 //   warps 0-3, 4-7   a tile each, a thread a row: the row's maximum, exponentials, sums; O is rescaled in tensor memory only when
 //                    a maximum has grown by more than 8 (powers of two: exactly)
-//   warps 8-11       8-bit values to halves (exactly) in shared memory, one block ahead in registers, two stages for K and for V
-//   warp 12          issues the MMAs
+//   warps 8-11       8-bit values to halves (exactly) in shared memory, K and V in turn, the other one's bytes under way; two stages for each
+//   warp 12          issues the MMAs (13-15 idle)
 // Scales, the tail and the weights are as in fa_q8_attn.cu with 2^7 in the place of 2^15, which leaves the maxima room to grow.  The blocks of all
 // tiles stand in a line that is cut into equal parts, one for each SM; the parts of a tile that is cut meet in the workspace, and a second kernel
 // joins them, spread over all SMs.
+// The loops of the roles share the instruction cache: what is unrolled (a row of scores in registers) is written once, the rest kept small.
 // Bound by the exponentials (16 a clock and SM: 2048 clocks for a block and 256 rows of any head dim) and, at 128 dims, by as many clocks of the tensor cores.
 #include "fa_q8.cuh"
 #include "fa_umma.cuh"
@@ -22,7 +23,10 @@ using namespace umma;
 
 constexpr int kRows = 256, kTok = 128;
 constexpr int kConv = 8, kMma = 12;                        // first converting warp, the issuing warp
-constexpr int kChunkThreads = 13 * 32;
+constexpr int kChunkThreads = 16 * 32;                     // (four warps have the same registers: three of the last four idle)
+// Registers of a thread of the four groups of warps; together those that the launch has (4 x 128): the weights keep a row of 128 scores.
+constexpr int kRegsRow = 176, kRegsConv = 104, kRegsMma = 56;
+static_assert(2 * kRegsRow + kRegsConv + kRegsMma == 4 * 128, "");
 constexpr int kScSlots = 4;                                // scales of blocks: a slot is free when the weights of the block two in front are done
 
 struct ChunkArgs {
@@ -130,12 +134,63 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
                  "r"(r[13]), "r"(r[14]), "r"(r[15])
                  : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
-    uint32_t r[16], q[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) { r[i] = __float_as_uint(v[i]); q[i] = __float_as_uint(v[16 + i]); }
-    tmem_st16(taddr, r);
-    tmem_st16(taddr + 16, q);
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\ntcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+// 32 columns without waiting for them.
+__device__ __forceinline__ void tmem_ld32_start(uint32_t taddr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Loads of read-only memory where `there` says so, zeros elsewhere, without a branch.
+__device__ __forceinline__ uint4 ld_if16(const uint8_t* p, bool there) {
+    uint4 r;
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %5, 0;\n mov.u32 %0, 0;\n mov.u32 %1, 0;\n mov.u32 %2, 0;\n mov.u32 %3, 0;\n @p ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];\n}\n"
+        : "=&r"(r.x), "=&r"(r.y), "=&r"(r.z), "=&r"(r.w)
+        : "l"(p), "r"((uint32_t)there));
+    return r;
+}
+__device__ __forceinline__ float ld_if(const float* p, bool there) {
+    float r;
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n mov.f32 %0, 0f00000000;\n @p ld.global.nc.f32 %0, [%1];\n}\n" : "=&f"(r) : "l"(p), "r"((uint32_t)there));
+    return r;
+}
+// Two floats as one operand of the packed instructions.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // D += A B with A (halves, two to a column) in tensor memory.
@@ -201,6 +256,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
 
     if (warp < kConv) {
         // ---- a tile's weights ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsRow));
         const int tile = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tmem_s[tile] + lanes, to = tmem_o[tile] + lanes;
@@ -238,7 +294,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
             const int last = there ? g.len - a.n_q + qi : -1;            // the last token that the row sees
             // the first token that some row of the warp does not see
             const int sure = __reduce_min_sync(0xffffffffu, there ? last : 0x7fffffff);
-            float m = kNegBig, mp = kNegBig, l = 0.f;
+            float m = kNegBig, mp = kNegBig;
+            f32x2 l = pack2(0.f, 0.f);                     // of the even and the odd tokens
             for (int i = g.i0; i < g.i1; ++i, ++blk, ++n_s) {
                 ok = mbar_wait(bar.s_full + tile, n_s & 1, &fail, status);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
@@ -246,79 +303,83 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                 const float2* scale = sc[blk % kScSlots];
                 const int t0 = i * kTok;
                 const bool edge = t0 + kTok - 1 > sure || sc_gone[blk % kScSlots];
+                if (edge) {                                // what is not seen becomes -infinity, in tensor memory
+#pragma unroll 1
+                    for (int u = 0; u < 8; ++u) {
+                        const int n = scale[u].y < 0.f ? 0 : last + 1 - (t0 + 16 * u);     // tokens that are seen
+                        uint32_t y[16];
+                        tmem_ld16(ts + 16 * u, y);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) y[j] = j < n ? y[j] : 0xff800000u;
+                        tmem_st16(ts + 16 * u, y);
+                    }
+                    tmem_st_wait();
+                }
+                float x[kTok];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32_start(ts + 32 * c, x + 32 * c);
+                float kf[8], sv[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const float2 k = scale[u];
+                    kf[u] = k.x * f;
+                    sv[u] = k.y;
+                    if (edge) {                            // (0 x -infinity; a scale that is NaN in tokens that the row does not see)
+                        const bool none = k.y < 0.f || t0 + 16 * u > last;
+                        kf[u] = none || kf[u] == 0.f ? 1.f : kf[u];
+                        sv[u] = none ? 0.f : sv[u];
+                    }
+                }
+                tmem_ld_wait();
                 // maxima of scores and of score + exponent of V's scale
                 float bm = kNegBig, bp = kNegBig;
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    float x[32];
-                    tmem_ld32(ts + 32 * c, x);
 #pragma unroll
-                    for (int hlf = 0; hlf < 2; ++hlf) {
-                        const float2 k = scale[2 * c + hlf];
-                        const float kf = k.x * f;
-                        float top;
-                        if (edge) {
-                            top = -INFINITY;
+                for (int u = 0; u < 8; ++u) {
+                    float top = x[16 * u];
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                const float y = x[16 * hlf + j] * kf;
-                                top = t0 + 32 * c + 16 * hlf + j <= last && !(k.y < 0.f) ? fmaxf(top, y) : top;
-                            }
-                        } else {
-                            top = x[16 * hlf];
-#pragma unroll
-                            for (int j = 1; j < 15; j += 2) top = fmaxf(top, fmaxf(x[16 * hlf + j], x[16 * hlf + j + 1]));
-                            top = fmaxf(top, x[16 * hlf + 15]) * kf;
-                        }
-                        bm = fmaxf(bm, top);
-                        bp = fmaxf(bp, top + (float)(exponent_of(k.y) + 1));
-                    }
+                    for (int j = 1; j < 15; j += 2) top = fmaxf(top, fmaxf(x[16 * u + j], x[16 * u + j + 1]));
+                    top = fmaxf(top, x[16 * u + 15]) * kf[u];
+                    bm = fmaxf(bm, top);
+                    bp = fmaxf(bp, top + (float)(exponent_of(sv[u]) + 1));
                 }
                 const bool grow = bm > m + 8.f || bp > mp + 8.f;
                 if (__any_sync(0xffffffffu, grow)) {
                     const float m2 = grow ? fmaxf(m, ceilf(bm)) : m, p2 = grow ? fmaxf(mp, ceilf(bp)) : mp;
-                    l *= pow2_down(m, m2);
-                    const float r = pow2_down(mp, p2);
+                    const float rl = pow2_down(m, m2), r = pow2_down(mp, p2);
+                    l = mul2(l, pack2(rl, rl));
                     m = m2;
                     mp = p2;
                     if (i > g.i0) {
 #pragma unroll 1
-                        for (int c = 0; c < D; c += 32) {
-                            float x[32];
-                            tmem_ld32(to + c, x);
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(to + c, o);
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) x[j] *= r;
-                            tmem_st32(to + c, x);
+                            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * r);
+                            tmem_st16(to + c, o);
                         }
-                        tmem_st_wait();
                     }
                 }
                 // weights: w = p sv 2^(m - m' + 7)
-#pragma unroll 1
+                const float d = fmaxf(m - mp + 7.f, -250.f);
+                const f32x2 neg = pack2(-m, -m);
+#pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    float x[32];
-                    tmem_ld32(ts + 32 * c, x);
                     uint32_t w[16];
 #pragma unroll
                     for (int hlf = 0; hlf < 2; ++hlf) {
-                        const float2 k = scale[2 * c + hlf];
-                        const float kf = k.x * f;
-                        const int e = (int)fminf(fmaxf(m - mp + 7.f, -250.f), (float)min(126, 125 - exponent_of(k.y)));
-                        const float cw = k.y * pow2i(e / 2) * pow2i(e - e / 2);
+                        const int u = 2 * c + hlf;
+                        const int e = (int)fminf(d, (float)min(126, 125 - exponent_of(sv[u])));
+                        const float cw = sv[u] * pow2i(e / 2) * pow2i(e - e / 2);
+                        const f32x2 k2 = pack2(kf[u], kf[u]), c2 = pack2(cw, cw);
 #pragma unroll
                         for (int j = 0; j < 16; j += 2) {
-                            float y0 = fmaf(x[16 * hlf + j], kf, -m), y1 = fmaf(x[16 * hlf + j + 1], kf, -m);
-                            bool o0 = false, o1 = false;
-                            if (edge) {
-                                const int t = t0 + 32 * c + 16 * hlf + j;
-                                o0 = !(t <= last) || k.y < 0.f;
-                                o1 = !(t + 1 <= last) || k.y < 0.f;
-                                y0 = o0 ? -INFINITY : y0;
-                                y1 = o1 ? -INFINITY : y1;
-                            }
-                            const float p0 = ex2(y0), p1 = ex2(y1);
-                            l += p0 + p1;
-                            w[8 * hlf + (j >> 1)] = half2_of(o0 ? 0.f : p0 * cw, o1 ? 0.f : p1 * cw);
+                            float y0, y1;
+                            unpack2(fma2(pack2(x[16 * u + j], x[16 * u + j + 1]), k2, neg), y0, y1);
+                            const f32x2 p = pack2(ex2(y0), ex2(y1));
+                            l = add2(l, p);
+                            unpack2(mul2(p, c2), y0, y1);
+                            w[8 * hlf + (j >> 1)] = half2_of(y0, y1);
                         }
                     }
                     tmem_st16(ts + 16 * c, w);
@@ -332,9 +393,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
             if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
             ++n_o;
             fence_after();
+            float l0, l1;
+            unpack2(l, l0, l1);
+            l0 += l1;
             if (g.i0 == 0 && g.i1 == g.n) {
                 const int e = (int)fminf(fmaxf(mp - m - 7.f, -250.f), 250.f);
-                const float f1 = pow2i(e / 2), f2 = pow2i(e - e / 2), r = l == 0.f ? 0.f : 1.f / l;
+                const float f1 = pow2i(e / 2), f2 = pow2i(e - e / 2), r = l0 == 0.f ? 0.f : 1.f / l0;
                 __nv_bfloat16* o = a.out + (((size_t)g.b * a.n_q + qi) * s.Hq + g.h * s.G + col % s.G) * D;
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
@@ -365,165 +429,195 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(o + c + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
                 }
-                *reinterpret_cast<float4*>(o + D) = make_float4(m, mp, l, 0.f);
+                *reinterpret_cast<float4*>(o + D) = make_float4(m, mp, l0, 0.f);
             }
             fence_before();                                // the next segment's MMAs come behind its first p_full
         }
     } else if (warp < kMma) {
         // ---- 8-bit values to halves ----
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConv));
         constexpr int kChunks = D / 16, kPass = 128 / kChunks, kPasses = kTok / kPass;       // 16-value chunks of a row; rows of a pass
         const int t = tid - kConv * 32, ch = t % kChunks, r0 = t / kChunks;
-        struct Raw { uint4 w[kPasses]; };
-        Raw kr, vr;
-        // the bytes of one side of block i of the segment (units of 16 tokens without a page, or in the tail: nothing)
-        auto load = [&](Raw& raw, const uint8_t* pages, const Seg& g, int i) {
-            const int paged = g.len >> s.lb << s.lb;
-            const int32_t* table = a.c.table + (size_t)g.b * s.nb;
-#pragma unroll
-            for (int p = 0; p < kPasses; ++p) {
-                const int tok = i * kTok + p * kPass + r0;
-                raw.w[p] = make_uint4(0u, 0u, 0u, 0u);
-                if (tok < paged) {
-                    const int page = __ldg(table + (tok >> s.lb));
-                    if (page >= 0 && page < s.n_pages)
-                        raw.w[p] = __ldg(reinterpret_cast<const uint4*>(pages + (((size_t)page * s.H + g.h) * (size_t)s.blk + (tok & (s.blk - 1))) * D + 16 * ch));
-                }
-            }
+        uint4 raw[kPasses];                                // of the step that comes: K of a block, then V
+        const unsigned char* tails[2] = {static_cast<const unsigned char*>(a.c.k_tail), static_cast<const unsigned char*>(a.c.v_tail)};
+        auto paged_of = [&](const Seg& g) { return g.len >> s.lb << s.lb; };
+        // Lanes 0-7: where 16 tokens of block i lie each, counted in 16 rows of the pages; kGone where no page is, kTail in the tail and
+        // behind the row's last token.
+        constexpr uint32_t kGone = 0xffffffffu, kTail = 0xfffffffeu;
+        auto pages_of = [&](const Seg& g, int i) {
+            const int tok = i * kTok + 16 * (lane & 7);
+            if (tok >= paged_of(g)) return kTail;
+            const int page = __ldg(a.c.table + (size_t)g.b * s.nb + (tok >> s.lb));
+            if (page < 0 || page >= s.n_pages) return kGone;
+            return (uint32_t)((((size_t)page * s.H + g.h) * (size_t)s.blk + (tok & (s.blk - 1))) >> 4);
         };
-        auto convert = [&](const Raw& raw, unsigned char* dst, const Seg& g, int i, int side) {
-            const int paged = g.len >> s.lb << s.lb;
-#pragma unroll
-            for (int p = 0; p < kPasses; ++p) {
-                const int r = p * kPass + r0, tok = i * kTok + r;
-                uint32_t h[8];
-                if (tok < paged || tok >= g.len) {
-                    const uint32_t w[4] = {raw.w[p].x, raw.w[p].y, raw.w[p].z, raw.w[p].w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t x = tok < paged ? q8_flip<FMT>(w[k]) : q8_flip<FMT>(0u);
-                        h[2 * k] = q8_halves<FMT>(x, 0);
-                        h[2 * k + 1] = q8_halves<FMT>(x, 1);
-                    }
-                } else {                                   // the tail: scaled by the power of two above its largest magnitude
-                    const uint32_t mx = __float_as_uint(a.c.tail_amax[((size_t)g.b * s.H + g.h) * 2 + side]);
-                    Vec16<__nv_bfloat16> v;
-                    if (mx < 0x7f800000u)
-                        v.load(reinterpret_cast<const __nv_bfloat16*>(side ? a.c.v_tail : a.c.k_tail) +
-                               (((size_t)g.b * s.H + g.h) * (size_t)s.blk + (tok - paged)) * D + 16 * ch);
-                    else v.zero();
-                    const float f = pow2i(13 - max((int)(mx >> 23) - 127, -100));
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) h[k] = half2_of(v.at(2 * k) * f, v.at(2 * k + 1) * f);
-                }
-                // (the upper half of the lanes of a row stores its second chunk first: no two meet in a bank)
-                const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
-                const bool swap = kChunks == 8 && ch >= 4;
-                *reinterpret_cast<uint4*>(dst + operand_offset(r, 2 * ch + (swap ? 1 : 0))) = swap ? hi : lo;
-                *reinterpret_cast<uint4*>(dst + operand_offset(r, 2 * ch + (swap ? 0 : 1))) = swap ? lo : hi;
-            }
-        };
-        // the scales of block i (threads 0 .. 7: 16 tokens each)
-        auto scales = [&](const Seg& g, int i, int slot) {
-            if (t >= 8) return;
-            const int tok = i * kTok + 16 * t, paged = g.len >> s.lb << s.lb;
-            float2 k = make_float2(0.f, 0.f);
-            bool gone = false;
-            if (tok < paged) {
-                const int page = __ldg(a.c.table + (size_t)g.b * s.nb + (tok >> s.lb));
-                if (page >= 0 && page < s.n_pages) {
-                    k = make_float2(__ldg(a.c.k_scale + (size_t)page * s.H + g.h), __ldg(a.c.v_scale + (size_t)page * s.H + g.h));
-                } else {
-                    gone = true;
-                    k.y = -1.f;
-                    q8_report(status, FA_ERR_INDEX);
-                }
-            } else if (tok < g.len) {
+        auto scales_of = [&](const Seg& g, int i, uint32_t at) {
+            const size_t ph = at >> (s.lb - 4);
+            float2 k = make_float2(ld_if(a.c.k_scale + ph, at < kTail), ld_if(a.c.v_scale + ph, at < kTail));
+            if (at == kGone) k.y = -1.f;
+            if (at == kTail && i * kTok + 16 * (lane & 7) < g.len) {
                 const float* am = a.c.tail_amax + ((size_t)g.b * s.H + g.h) * 2;
                 const uint32_t km = __float_as_uint(am[0]), vm = __float_as_uint(am[1]);
                 k.x = km >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : pow2i(max((int)(km >> 23) - 127, -100) - 13);
                 k.y = vm >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : pow2i(max((int)(vm >> 23) - 127, -100) - 13);
             }
-            sc[slot][t] = k;
-            const unsigned any = __ballot_sync(0xffu, gone);
-            if (t == 0) sc_gone[slot] = any != 0;
+            return k;
+        };
+        const uint32_t lane_at = (uint32_t)((r0 & 15) * D + 16 * ch);
+        auto in_pages = [&](const Seg& g, int i) { return (i + 1) * kTok <= paged_of(g); };      // the block, as a whole (others are read when they are converted)
+        auto fetch = [&](int p, const uint8_t* side, uint32_t pages, bool there) {
+            const uint32_t at = __shfl_sync(0xffffffffu, pages, (p * kPass + r0) >> 4);
+            raw[p] = ld_if16(side + (size_t)at * (16 * D) + lane_at, there && at < kTail);
+        };
+        // (the upper half of the lanes of a row stores its second chunk first: no two meet in a bank)
+        const bool swap = kChunks == 8 && ch >= 4;
+        auto put = [&](unsigned char* dst, int r, const uint32_t (&h)[8]) {
+            const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
+            *reinterpret_cast<uint4*>(dst + operand_offset(r, 2 * ch + (swap ? 1 : 0))) = swap ? hi : lo;
+            *reinterpret_cast<uint4*>(dst + operand_offset(r, 2 * ch + (swap ? 0 : 1))) = swap ? lo : hi;
+        };
+        auto halves = [&](const uint4& x, uint32_t (&h)[8]) {
+            const uint32_t w[4] = {q8_flip<FMT>(x.x), q8_flip<FMT>(x.y), q8_flip<FMT>(x.z), q8_flip<FMT>(x.w)};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                h[2 * k] = q8_halves<FMT>(w[k], 0);
+                h[2 * k + 1] = q8_halves<FMT>(w[k], 1);
+            }
         };
         bool more = line.next(a, g);
+        uint32_t pages = kTail;
+        float2 scale = make_float2(0.f, 0.f);
         if (more) {
-            load(kr, a.c.k_pages, g, g.i0);
-            load(vr, a.c.v_pages, g, g.i0);
+            pages = pages_of(g, g.i0);
+            scale = scales_of(g, g.i0, pages);
+#pragma unroll
+            for (int p = 0; p < kPasses; ++p) fetch(p, a.c.k_pages, pages, in_pages(g, g.i0));
         }
         while (ok && more) {
             Seg nx = g;
             for (int i = g.i0; i < g.i1; ++i, ++blk) {
                 const uint32_t st = blk & 1, ph = (blk >> 1) & 1;
+                const bool inside = in_pages(g, i);
                 if (i + 1 == g.i1) more = line.next(a, nx);
-                const int ni = i + 1 < g.i1 ? i + 1 : nx.i0;
-                const Seg& ng = i + 1 < g.i1 ? g : nx;
                 const bool go = i + 1 < g.i1 || more;
-                if (blk >= 2 && !(ok = mbar_wait(bar.k_empty + st, ph ^ 1, &fail, status))) break;
-                scales(g, i, (int)(blk % kScSlots));
-                convert(kr, ks + st * kTile, g, i, 0);
-                fence_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar.k_full + st);
-                if (go) load(kr, a.c.k_pages, ng, ni);
-                if (blk >= 2 && !(ok = mbar_wait(bar.v_empty + st, ph ^ 1, &fail, status))) break;
-                convert(vr, vs + st * kTile, g, i, 1);
-                fence_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar.v_full + st);
-                if (go) load(vr, a.c.v_pages, ng, ni);
+                const int ni = i + 1 < g.i1 ? i + 1 : nx.i0;                // (nx is g within the segment)
+                const uint32_t npages = go ? pages_of(nx, ni) : kTail;
+                const bool ninside = go && in_pages(nx, ni);
+                float2 nscale = make_float2(0.f, 0.f);
+#pragma unroll 1
+                for (int side = 0; side < 2; ++side) {
+                    if (blk >= 2) ok = mbar_wait((side ? bar.v_empty : bar.k_empty) + st, ph ^ 1, &fail, status);
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                    if (side == 0 && warp == kConv) {
+                        const unsigned gone = __ballot_sync(0xffffffffu, pages == kGone);
+                        if (lane < 8) sc[blk % kScSlots][lane] = scale;
+                        if (lane == 0) {
+                            sc_gone[blk % kScSlots] = gone != 0;
+                            if (gone) q8_report(status, FA_ERR_INDEX);
+                        }
+                    }
+                    if (side == 0) nscale = scales_of(nx, ni, go ? npages : kGone);
+                    unsigned char* dst = (side ? vs : ks) + st * kTile;
+                    const uint8_t* next_side = side ? a.c.k_pages : a.c.v_pages;
+                    const uint32_t next_pages = side ? npages : pages;
+                    const bool next_inside = side ? ninside : inside;
+                    if (inside) {
+#pragma unroll
+                        for (int p = 0; p < kPasses; ++p) {
+                            uint32_t h[8];
+                            halves(raw[p], h);
+                            fetch(p, next_side, next_pages, next_inside);
+                            put(dst, p * kPass + r0, h);
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int p = 0; p < kPasses; ++p) {
+                            const int r = p * kPass + r0, tok = i * kTok + r;
+                            const uint32_t at = __shfl_sync(0xffffffffu, pages, r >> 4);
+                            uint32_t h[8];
+                            if (at == kTail && tok < g.len) {      // the tail: scaled by the power of two above its largest magnitude
+                                const uint32_t mx = __float_as_uint(a.c.tail_amax[((size_t)g.b * s.H + g.h) * 2 + side]);
+                                Vec16<__nv_bfloat16> v;
+                                if (mx < 0x7f800000u)
+                                    v.load(reinterpret_cast<const __nv_bfloat16*>(tails[side]) +
+                                           (((size_t)g.b * s.H + g.h) * (size_t)s.blk + (tok - paged_of(g))) * D + 16 * ch);
+                                else v.zero();
+                                const float f = pow2i(13 - max((int)(mx >> 23) - 127, -100));
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) h[k] = half2_of(v.at(2 * k) * f, v.at(2 * k + 1) * f);
+                            } else if (at < kTail) {
+                                halves(ld_if16((side ? a.c.v_pages : a.c.k_pages) + (size_t)at * (16 * D) + lane_at, true), h);
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) h[k] = 0u;
+                            }
+                            put(dst, r, h);
+                        }
+#pragma unroll
+                        for (int p = 0; p < kPasses; ++p) fetch(p, next_side, next_pages, next_inside);
+                    }
+                    fence_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive((side ? bar.v_full : bar.k_full) + st);
+                }
+                if (!ok) break;
+                pages = npages;
+                scale = nscale;
             }
             g = nx;
         }
     } else {
         // ---- the MMAs ----
-        const uint32_t q_addr = smem_u32(qs), k_addr = smem_u32(ks), v_addr = smem_u32(vs);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsMma));
+        // operands: K-major with 64 dims to a row of 128 bytes, the next 64 a box further; V the same read along the tokens (MN-major)
+        const uint64_t qd0 = umma_desc(smem_u32(qs), 1, 1024 >> 4), kd0 = umma_desc(smem_u32(ks), 1, 1024 >> 4);
+        const uint64_t vd0 = umma_desc(smem_u32(vs), (kTok * 128) >> 4, 1024 >> 4);
         uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0};         // phases of p_full, q_full
-        while (ok && line.next(a, g)) {
+        while (warp == kMma && ok && line.next(a, g)) {
             const int tiles = two_tiles(g) ? 2 : 1;
             const int n = g.i1 - g.i0;
-            auto scores = [&](int t, uint32_t b) {
-                if (lane == 0) {
-                    const uint32_t st = b & 1;
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t off = (uint32_t)((k >> 2) * (kTok * 128) + (k & 3) * 32);
-                        umma_bf16(tmem_s[t], umma_desc(q_addr + t * kTile + off, 1, 1024 >> 4), umma_desc(k_addr + st * kTile + off, 1, 1024 >> 4), kIdescS, k > 0);
-                    }
-                    umma_commit(bar.s_full + t);
-                }
-                __syncwarp();
-            };
             for (int t = 0; t < tiles && ok; ++t) ok = mbar_wait(bar.q_full + t, n_q[t]++ & 1, &fail, status);
-            if (!ok || !(ok = mbar_wait(bar.k_full + (blk & 1), (blk >> 1) & 1, &fail, status))) break;
-            fence_after();
-            for (int t = 0; t < tiles; ++t) scores(t, blk);
-            if (lane == 0) umma_commit(bar.k_empty + (blk & 1));
-            for (int i = 0; i < n; ++i, ++blk) {
-                const uint32_t st = blk & 1;
-                const bool more = i + 1 < n;
-                if (more && !(ok = mbar_wait(bar.k_full + (st ^ 1), ((blk + 1) >> 1) & 1, &fail, status))) break;
-                if (!(ok = mbar_wait(bar.v_full + st, (blk >> 1) & 1, &fail, status))) break;
-                for (int t = 0; t < tiles; ++t) {
-                    if (!(ok = mbar_wait(bar.p_full + t, n_p[t]++ & 1, &fail, status))) break;
-                    fence_after();
-                    if (lane == 0) {
+            // step i: the outputs of block i - 1, then the scores of block i, for each tile
+#pragma unroll 1
+            for (int i = 0; i <= n && ok; ++i) {
+                const uint32_t bk = blk + i, bv = bk - 1;
+                if (i < n) ok = mbar_wait(bar.k_full + (bk & 1), (bk >> 1) & 1, &fail, status);
+                if (ok && i > 0) ok = mbar_wait(bar.v_full + (bv & 1), (bv >> 1) & 1, &fail, status);
+                const uint64_t kd = kd0 + (uint64_t)((bk & 1) * kTile >> 4), vd = vd0 + (uint64_t)((bv & 1) * kTile >> 4);
+#pragma unroll 1
+                for (int t = 0; t < tiles && ok; ++t) {
+                    if (i > 0) {
+                        if (!(ok = mbar_wait(bar.p_full + t, n_p[t]++ & 1, &fail, status))) break;
+                        fence_after();
+                        if (lane == 0) {
+                            const uint32_t p = tmem + 128 * t, o = tmem + 256 + D * t;
 #pragma unroll
-                        for (int k = 0; k < kTok / 16; ++k)
-                            umma_ts(tmem_o[t], tmem_s[t] + 8 * k, umma_desc(v_addr + st * kTile + k * 2048, (kTok * 128) >> 4, 1024 >> 4), kIdescO, i > 0 || k > 0);
-                        if (!more) umma_commit(bar.o_done + t);
+                            for (int k = 0; k < kTok / 16; ++k) umma_ts(o, p + 8 * k, vd + (uint64_t)(k * 2048 >> 4), kIdescO, i > 1 || k > 0);
+                            if (i == n) umma_commit(bar.o_done + t);
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
-                    if (more) scores(t, blk + 1);
+                    if (i < n) {
+                        fence_after();
+                        if (lane == 0) {
+                            const uint64_t qd = qd0 + (uint64_t)(t * kTile >> 4);
+#pragma unroll
+                            for (int k = 0; k < D / 16; ++k) {
+                                const uint64_t off = (uint64_t)(((k >> 2) * (kTok * 128) + (k & 3) * 32) >> 4);
+                                umma_bf16(tmem + 128 * t, qd + off, kd + off, kIdescS, k > 0);
+                            }
+                            umma_commit(bar.s_full + t);
+                        }
+                        __syncwarp();
+                    }
                 }
-                if (!ok) break;
-                if (lane == 0) {
-                    umma_commit(bar.v_empty + st);
-                    if (more) umma_commit(bar.k_empty + (st ^ 1));
+                if (ok && lane == 0) {
+                    if (i > 0) umma_commit(bar.v_empty + (bv & 1));
+                    if (i < n) umma_commit(bar.k_empty + (bk & 1));
                 }
                 __syncwarp();
             }
+            blk += n;
         }
     }
     fence_before();
