@@ -4,15 +4,20 @@
 // A CTA takes 256 rows, a row being one (query, query head) of a KV head, as two tiles of 128, over blocks of 128 tokens.  Per block and tile:
 // S = Q K^T (accumulators), the weights P of the softmax rounded to halves in the place of S, O += P V with P read from
 // tensor memory.  The two tiles take turns: the tensor cores work for one while the other's weights are formed.
-//   warps 0-3, 4-7   a tile each, a thread a row: the row's maximum, exponentials, sums; O is rescaled in tensor memory only when
-//                    a maximum has grown by more than 8 (powers of two: exactly)
-//   warps 8-11       8-bit values to halves (exactly) in shared memory, K and V in turn, the other one's bytes under way; two stages for each
-//   warp 12          issues the MMAs (13-15 idle)
-// Scales, the tail and the weights are as in fa_q8_attn.cu with 2^7 in the place of 2^15, which leaves the maxima room to grow.  The blocks of all
+//   warps 0-7, 8-15  a tile each, two threads to a row with 64 of the block's tokens each: the row's maximum (exchanged), exponentials,
+//                    sums; O is rescaled in tensor memory only when a maximum has grown by more than 8 (powers of two: exactly).  (One thread to a row, its 128
+//                    scores in registers, took 6000 clocks a block: two warps to a scheduler do not cover their own latencies.)
+//   warps 16-19, 21-23  8-bit values to halves (exactly) in shared memory, K and V in turn, the other one's bytes under way; two stages for each
+//   warp 20          issues the MMAs
+// Scales, the tail and the weights are as in fa_q8_attn.cu with 2^7 in the place of 2^15, which leaves the maxima room to grow; a weight is one exponential, of
+// score + log2 of V's scale - m' + 7, and 16 tokens' sum of weights becomes their sum of p by one factor.  int8 K values are taken as q + 128 in the place of
+// a half's last bits (that is (q + 128) 2^-24, exactly): two instructions less a value; 128 times the sum of the row's q is subtracted from the scores.  The blocks of all
 // tiles stand in a line that is cut into equal parts, one for each SM; the parts of a tile that is cut meet in the workspace, and a second kernel
 // joins them, spread over all SMs.
 // The loops of the roles share the instruction cache: what is unrolled (a row of scores in registers) is written once, the rest kept small.
 // Bound by the exponentials (16 a clock and SM: 2048 clocks for a block and 256 rows of any head dim) and, at 128 dims, by as many clocks of the tensor cores.
+#include <type_traits>
+
 #include "fa_q8.cuh"
 #include "fa_umma.cuh"
 
@@ -22,11 +27,11 @@ namespace {
 using namespace umma;
 
 constexpr int kRows = 256, kTok = 128;
-constexpr int kConv = 8, kMma = 12;                        // first converting warp, the issuing warp
-constexpr int kChunkThreads = 16 * 32;                     // (four warps have the same registers: three of the last four idle)
-// Registers of a thread of the four groups of warps; together those that the launch has (4 x 128): the weights keep a row of 128 scores.
-constexpr int kRegsRow = 176, kRegsConv = 104, kRegsMma = 56;
-static_assert(2 * kRegsRow + kRegsConv + kRegsMma == 4 * 128, "");
+constexpr int kConv = 16, kMma = 20, kConvWarps = 7;       // first converting warp, the issuing warp, converting warps (16-19, 21-23)
+constexpr int kChunkThreads = 24 * 32;
+// Registers of a thread of the weights and of the others; together those that the launch has (6 groups of four warps x 80).
+constexpr int kRegsRow = 80, kRegsRest = 80;
+static_assert(4 * kRegsRow + 2 * kRegsRest == 6 * 80, "");
 constexpr int kScSlots = 4;                                // scales of blocks: a slot is free when the weights of the block two in front are done
 
 struct ChunkArgs {
@@ -54,7 +59,6 @@ __device__ __forceinline__ uint32_t half2_of(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
 
 // Tokens of row b that the cache holds; those that column tile ct sees, in blocks of 128.
 __device__ __forceinline__ int row_len(const ChunkArgs& a, int b) {
@@ -142,33 +146,6 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
         : "r"(taddr)
         : "memory");
 }
-// 32 columns without waiting for them.
-__device__ __forceinline__ void tmem_ld32_start(uint32_t taddr, float* v) {
-    uint32_t* r = reinterpret_cast<uint32_t*>(v);
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-// Loads of read-only memory where `there` says so, zeros elsewhere, without a branch.
-__device__ __forceinline__ uint4 ld_if16(const uint8_t* p, bool there) {
-    uint4 r;
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.u32 p, %5, 0;\n mov.u32 %0, 0;\n mov.u32 %1, 0;\n mov.u32 %2, 0;\n mov.u32 %3, 0;\n @p ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];\n}\n"
-        : "=&r"(r.x), "=&r"(r.y), "=&r"(r.z), "=&r"(r.w)
-        : "l"(p), "r"((uint32_t)there));
-    return r;
-}
-__device__ __forceinline__ float ld_if(const float* p, bool there) {
-    float r;
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n mov.f32 %0, 0f00000000;\n @p ld.global.nc.f32 %0, [%1];\n}\n" : "=&f"(r) : "l"(p), "r"((uint32_t)there));
-    return r;
-}
 // Two floats as one operand of the packed instructions.
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 pack2(float a, float b) {
@@ -203,8 +180,16 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// Row r, 16-byte chunk c (8 dims) of a K-major or MN-major operand of D dims: 64 dims to a 128-byte row, chunks permuted by the row.
-__device__ __forceinline__ int operand_offset(int r, int c) { return (c >> 3) * (kTok * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
+// Row r, dims 8 c .. 8 c + 7 of an operand of D dims: 64 dims to a 128-byte row, its 16-byte chunks permuted by the row.  With 128 dims the even c come first,
+// then the odd ones, in q, K and V alike (and so in the columns of O): the lanes that store a row's chunks then meet all banks.
+template <int D>
+__device__ __forceinline__ int operand_offset(int r, int c) {
+    const int at = D == 128 ? (c >> 1) + 8 * (c & 1) : c;
+    return (at >> 3) * (kTok * 128) + r * 128 + (((at & 7) ^ (r & 7)) << 4);
+}
+// First of the 8 dims that columns 8 at .. 8 at + 7 of O are.
+template <int D>
+__device__ __forceinline__ int dim_of(int at) { return D == 128 ? 16 * (at & 7) + 8 * (at >> 3) : 8 * at; }
 
 struct Bars {
     uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], p_full[2], o_done[2];
@@ -219,8 +204,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     unsigned char *qs = smem, *ks = smem + 2 * kTile, *vs = smem + 4 * kTile;
     __shared__ Bars bar;
-    __shared__ float2 sc[kScSlots][8];                     // K and V scale of 16 tokens each; a V scale below zero: they have no page
-    __shared__ int sc_gone[kScSlots];
+    __shared__ float2 sc[kScSlots][8];                     // K scale (NaN if V's is) and log2 of V's scale of 16 tokens each
+    __shared__ int sc_marks[kScSlots];                     // bit u: 16 tokens that have no page; bit 8 + u: in the tail
+    __shared__ float2 meet[2][2][2][128];                  // what the two threads of a row tell each other: [turn][tile][half][row]
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int fail;
     const Q8Dims& s = a.s;
@@ -229,8 +215,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
     asm volatile("griddepcontrol.launch_dependents;");
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar.k_full + i, 4); mbar_init(bar.k_empty + i, 1); mbar_init(bar.v_full + i, 4); mbar_init(bar.v_empty + i, 1);
-            mbar_init(bar.q_full + i, 4); mbar_init(bar.s_full + i, 1); mbar_init(bar.p_full + i, 4); mbar_init(bar.o_done + i, 1);
+            mbar_init(bar.k_full + i, kConvWarps); mbar_init(bar.k_empty + i, 1); mbar_init(bar.v_full + i, kConvWarps); mbar_init(bar.v_empty + i, 1);
+            mbar_init(bar.q_full + i, 8); mbar_init(bar.s_full + i, 1); mbar_init(bar.p_full + i, 8); mbar_init(bar.o_done + i, 1);
         }
         fail = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -254,39 +240,60 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
     uint32_t blk = 0;                                      // blocks so far: stages and phases
     bool ok = true;
 
-    if (warp < kConv) {
+    if (warp < 16) {
         // ---- a tile's weights ----
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsRow));
-        const int tile = warp >> 2, row = tid & 127;
+        const int tile = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t ts = tmem_s[tile] + lanes, to = tmem_o[tile] + lanes;
-        uint32_t n_s = 0, n_o = 0;                         // phases of s_full, o_done
+        // this thread's scores, whose place its weights take (two to a column), and its half of the columns of O
+        const uint32_t ts = tmem_s[tile] + lanes + 64 * half, to = tmem_o[tile] + lanes + (D / 2) * half;
+        uint32_t n_s = 0, n_o = 0, turn = 0;               // phases of s_full, o_done; turns of `meet`
+        // Both threads of a row: what the other one says.  (Two turns' places: a place is written again when both are past the turn between.)
+        auto tell = [&](float2 v) {
+            meet[turn & 1][tile][half][row] = v;
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + tile * 4 + (warp & 3)) : "memory");
+            v = meet[turn & 1][tile][half ^ 1][row];
+            ++turn;
+            return v;
+        };
         while (ok && line.next(a, g)) {
             if (tile == 1 && !two_tiles(g)) { blk += g.i1 - g.i0; continue; }
             const int col = g.ct * kRows + tile * 128 + row, qi = col / s.G;
             const bool there = qi < a.n_q;
-            // q: scaled by a power of two to halves, into shared memory
-            const int64_t qoff = (int64_t)g.b * a.sb + (int64_t)qi * a.si + (int64_t)(g.h * s.G + col % s.G) * a.sg;
-            Vec16<__nv_bfloat16> v[D / 16];
-            uint32_t mx = 0;
+            // q: scaled by a power of two to halves, into shared memory; a thread has half of the dims
+            float f, shift;
+            {
+                const __nv_bfloat16* qp = a.q + (int64_t)g.b * a.sb + (int64_t)qi * a.si + (int64_t)(g.h * s.G + col % s.G) * a.sg + (D / 2) * half;
+                Vec16<__nv_bfloat16> v[D / 32];
+                uint32_t mx = 0;
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-                if (there) v[c].load(a.q + qoff + 16 * c);
-                else v[c].zero();
-                mx = max(mx, v[c].amax_bits());
-            }
-            const int eq = max((int)(mx >> 23) - 127, -100);
-            const float fq = pow2i(13 - eq), f = pow2i(eq - 13) * (s.scale * kLog2e);
+                for (int c = 0; c < D / 32; ++c) {
+                    if (there) v[c].load(qp + 16 * c);
+                    else v[c].zero();
+                    mx = max(mx, v[c].amax_bits());
+                }
+                mx = max(mx, __float_as_uint(tell(make_float2(__uint_as_float(mx), 0.f)).x));
+                const int eq = max((int)(mx >> 23) - 127, -100);
+                const float fq = pow2i(13 - eq);
+                f = pow2i(eq - 13) * (s.scale * kLog2e);
+                float sum = 0.f;
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
-                uint4 w;
-                const int e = 8 * (c & 1);
-                w.x = half2_of(v[c >> 1].at(e) * fq, v[c >> 1].at(e + 1) * fq);
-                w.y = half2_of(v[c >> 1].at(e + 2) * fq, v[c >> 1].at(e + 3) * fq);
-                w.z = half2_of(v[c >> 1].at(e + 4) * fq, v[c >> 1].at(e + 5) * fq);
-                w.w = half2_of(v[c >> 1].at(e + 6) * fq, v[c >> 1].at(e + 7) * fq);
-                *reinterpret_cast<uint4*>(qs + tile * kTile + operand_offset(row, c)) = w;
+                for (int c = 0; c < D / 16; ++c) {
+                    float y[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        y[k] = v[c >> 1].at(8 * (c & 1) + k) * fq;
+                        sum += y[k];                       // (as the halves have it, but for values below 2^-29 of the largest)
+                    }
+                    *reinterpret_cast<uint4*>(qs + tile * kTile + operand_offset<D>(row, half * (D / 16) + c)) =
+                        make_uint4(half2_of(y[0], y[1]), half2_of(y[2], y[3]), half2_of(y[4], y[5]), half2_of(y[6], y[7]));
+                }
+                const float other = tell(make_float2(sum, 0.f)).x;
+                sum = half ? other + sum : sum + other;    // (the same bits in both)
+                // a product of int8 K is (q + 128) 2^-24 times q: score = (product - shift) x scale
+                shift = FMT == FA_Q8_INT8 ? 128.f * sum : 0.f;
             }
+            constexpr float grain = FMT == FA_Q8_INT8 ? 0x1p24f : 1.f;
             fence_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar.q_full + tile);
@@ -295,18 +302,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
             // the first token that some row of the warp does not see
             const int sure = __reduce_min_sync(0xffffffffu, there ? last : 0x7fffffff);
             float m = kNegBig, mp = kNegBig;
-            f32x2 l = pack2(0.f, 0.f);                     // of the even and the odd tokens
-            for (int i = g.i0; i < g.i1; ++i, ++blk, ++n_s) {
-                ok = mbar_wait(bar.s_full + tile, n_s & 1, &fail, status);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                fence_after();
-                const float2* scale = sc[blk % kScSlots];
-                const int t0 = i * kTok;
-                const bool edge = t0 + kTok - 1 > sure || sc_gone[blk % kScSlots];
-                if (edge) {                                // what is not seen becomes -infinity, in tensor memory
+            f32x2 l = pack2(0.f, 0.f);                     // of the even and the odd tokens of this half
+            // The weights of block i.  edge: some row of the warp does not see all of its tokens, or some of them are in the tail.
+            auto weights = [&](auto edge_of, const float2* scale, int marks, int i) {
+                constexpr bool edge = decltype(edge_of)::value;
+                const int t0 = i * kTok + 64 * half;
+                if constexpr (edge) {                      // what is not seen becomes -infinity, in tensor memory
 #pragma unroll 1
-                    for (int u = 0; u < 8; ++u) {
-                        const int n = scale[u].y < 0.f ? 0 : last + 1 - (t0 + 16 * u);     // tokens that are seen
+                    for (int u = 0; u < 4; ++u) {
+                        const int n = marks >> u & 1 ? 0 : last + 1 - (t0 + 16 * u);       // tokens that are seen
                         uint32_t y[16];
                         tmem_ld16(ts + 16 * u, y);
 #pragma unroll
@@ -315,33 +319,45 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                     }
                     tmem_st_wait();
                 }
-                float x[kTok];
+                // Of 16 tokens: score = product x kf + off; log2 of V's scale.
+                float kf[4], off[4], lv[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld32_start(ts + 32 * c, x + 32 * c);
-                float kf[8], sv[8];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
+                for (int u = 0; u < 4; ++u) {
                     const float2 k = scale[u];
-                    kf[u] = k.x * f;
-                    sv[u] = k.y;
-                    if (edge) {                            // (0 x -infinity; a scale that is NaN in tokens that the row does not see)
-                        const bool none = k.y < 0.f || t0 + 16 * u > last;
-                        kf[u] = none || kf[u] == 0.f ? 1.f : kf[u];
-                        sv[u] = none ? 0.f : sv[u];
+                    float kk = k.x * f;
+                    kf[u] = kk * grain;
+                    off[u] = -kk * shift;
+                    if constexpr (edge) {                  // tokens that are not seen, in whatever scale; 0 x -infinity; the tail's products have no shift
+                        const bool none = (marks >> u & 1) || t0 + 16 * u > last, tail = marks >> (8 + u) & 1;
+                        kk = none ? 1.f : kk == 0.f ? 0x1p-100f : kk;
+                        kf[u] = tail ? kk : kk * grain;
+                        off[u] = none || tail ? 0.f : -kk * shift;
                     }
+                    lv[u] = k.y;
                 }
-                tmem_ld_wait();
-                // maxima of scores and of score + exponent of V's scale
+                // maxima of scores and of score + log2 of V's scale
                 float bm = kNegBig, bp = kNegBig;
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    float top = x[16 * u];
+                for (int c = 0; c < 2; ++c) {
+                    float x[32], top[2];
+                    tmem_ld32(ts + 32 * c, x);
 #pragma unroll
-                    for (int j = 1; j < 15; j += 2) top = fmaxf(top, fmaxf(x[16 * u + j], x[16 * u + j + 1]));
-                    top = fmaxf(top, x[16 * u + 15]) * kf[u];
-                    bm = fmaxf(bm, top);
-                    bp = fmaxf(bp, top + (float)(exponent_of(sv[u]) + 1));
+                    for (int h2 = 0; h2 < 2; ++h2) {
+                        const float* y = x + 16 * h2;
+                        const float p = fmaxf(fmaxf(y[0], y[1]), y[2]), q = fmaxf(fmaxf(y[3], y[4]), y[5]), r = fmaxf(fmaxf(y[6], y[7]), y[8]);
+                        const float w = fmaxf(fmaxf(y[9], y[10]), y[11]), v = fmaxf(fmaxf(y[12], y[13]), y[14]);
+                        top[h2] = fmaxf(fmaxf(fmaxf(p, q), fmaxf(r, w)), fmaxf(v, y[15]));
+                    }
+#pragma unroll
+                    for (int h2 = 0; h2 < 2; ++h2) {
+                        const float y = fmaf(top[h2], kf[2 * c + h2], off[2 * c + h2]);
+                        bm = fmaxf(bm, y);
+                        bp = fmaxf(bp, y + lv[2 * c + h2]);
+                    }
                 }
+                const float2 other = tell(make_float2(bm, bp));
+                bm = fmaxf(bm, other.x);
+                bp = fmaxf(bp, other.y);
                 const bool grow = bm > m + 8.f || bp > mp + 8.f;
                 if (__any_sync(0xffffffffu, grow)) {
                     const float m2 = grow ? fmaxf(m, ceilf(bm)) : m, p2 = grow ? fmaxf(mp, ceilf(bp)) : mp;
@@ -351,7 +367,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                     mp = p2;
                     if (i > g.i0) {
 #pragma unroll 1
-                        for (int c = 0; c < D; c += 16) {
+                        for (int c = 0; c < D / 2; c += 16) {
                             uint32_t o[16];
                             tmem_ld16(to + c, o);
 #pragma unroll
@@ -360,30 +376,40 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                         }
                     }
                 }
-                // weights: w = p sv 2^(m - m' + 7)
-                const float d = fmaxf(m - mp + 7.f, -250.f);
-                const f32x2 neg = pack2(-m, -m);
+                // weights: w = p sv 2^(m - m' + 7); below 2^-100 p they are none, and p is what the sum needs
+                const float d = m - mp + 7.f;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < 2; ++c) {
                     uint32_t w[16];
+                    float x[32];
+                    tmem_ld32(ts + 32 * c, x);                       // (again: they would not all stay in registers)
 #pragma unroll
-                    for (int hlf = 0; hlf < 2; ++hlf) {
-                        const int u = 2 * c + hlf;
-                        const int e = (int)fminf(d, (float)min(126, 125 - exponent_of(sv[u])));
-                        const float cw = sv[u] * pow2i(e / 2) * pow2i(e - e / 2);
-                        const f32x2 k2 = pack2(kf[u], kf[u]), c2 = pack2(cw, cw);
+                    for (int h2 = 0; h2 < 2; ++h2) {
+                        const int u = 2 * c + h2;
+                        const float e = fmaxf(lv[u] + d, -100.f), back = ex2(-e), z = off[u] + (e - m);
+                        const f32x2 k2 = pack2(kf[u], kf[u]), z2 = pack2(z, z);
+                        f32x2 sum = pack2(0.f, 0.f);
 #pragma unroll
                         for (int j = 0; j < 16; j += 2) {
                             float y0, y1;
-                            unpack2(fma2(pack2(x[16 * u + j], x[16 * u + j + 1]), k2, neg), y0, y1);
-                            const f32x2 p = pack2(ex2(y0), ex2(y1));
-                            l = add2(l, p);
-                            unpack2(mul2(p, c2), y0, y1);
-                            w[8 * hlf + (j >> 1)] = half2_of(y0, y1);
+                            unpack2(fma2(pack2(x[16 * h2 + j], x[16 * h2 + j + 1]), k2, z2), y0, y1);
+                            y0 = ex2(y0);
+                            y1 = ex2(y1);
+                            sum = add2(sum, pack2(y0, y1));
+                            w[8 * h2 + (j >> 1)] = half2_of(y0, y1);
                         }
+                        l = fma2(sum, pack2(back, back), l);
                     }
                     tmem_st16(ts + 16 * c, w);
                 }
+            };
+            for (int i = g.i0; i < g.i1; ++i, ++blk, ++n_s) {
+                ok = mbar_wait(bar.s_full + tile, n_s & 1, &fail, status);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                fence_after();
+                const int marks = sc_marks[blk % kScSlots] >> (4 * half);           // (bits 0-3 and 8-11 are this half's)
+                if (i * kTok + 64 * half + 63 > sure || (marks & 0xf0f)) weights(std::true_type(), sc[blk % kScSlots] + 4 * half, marks, i);
+                else weights(std::false_type(), sc[blk % kScSlots] + 4 * half, marks, i);
                 tmem_st_wait();
                 fence_before();
                 __syncwarp();
@@ -396,49 +422,51 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
             float l0, l1;
             unpack2(l, l0, l1);
             l0 += l1;
-            if (g.i0 == 0 && g.i1 == g.n) {
-                const int e = (int)fminf(fmaxf(mp - m - 7.f, -250.f), 250.f);
-                const float f1 = pow2i(e / 2), f2 = pow2i(e - e / 2), r = l0 == 0.f ? 0.f : 1.f / l0;
-                __nv_bfloat16* o = a.out + (((size_t)g.b * a.n_q + qi) * s.Hq + g.h * s.G + col % s.G) * D;
+            l1 = tell(make_float2(l0, 0.f)).x;
+            l0 = half ? l1 + l0 : l0 + l1;
+            const int e = (int)fminf(fmaxf(mp - m - 7.f, -250.f), 250.f);
+            const float f1 = pow2i(e / 2), f2 = pow2i(e - e / 2), r = l0 == 0.f ? 0.f : 1.f / l0;
+            const bool lone = g.i0 == 0 && g.i1 == g.n;
+            __nv_bfloat16* o = a.out + (((size_t)g.b * a.n_q + qi) * s.Hq + g.h * s.G + col % s.G) * D;
+            // parts of a tile lie one behind the other from 2 x its first CTA + 1 on (as in fa_q8_attn.cu)
+            float* part = a.part + ((size_t)(g.u / line.per + 1 + blockIdx.x) * kRows + tile * 128 + row) * (D + 4);
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    float x[32];
-                    tmem_ld32(to + c, x);
-                    if (there) {
+            for (int c = 0; c < D / 2; c += 16) {
+                uint32_t x[16];
+                tmem_ld16(to + c, x);
+                const int at = ((D / 2) * half + c) >> 3;
 #pragma unroll
-                        for (int j = 0; j < 32; j += 8) {
-                            uint32_t w[4];
+                for (int j = 0; j < 2; ++j) {
+                    float y[8];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const __nv_bfloat162 h = __floats2bfloat162_rn(x[j + 2 * k] * r * f1 * f2, x[j + 2 * k + 1] * r * f1 * f2);
-                                w[k] = *reinterpret_cast<const uint32_t*>(&h);
-                            }
-                            *reinterpret_cast<uint4*>(o + c + j) = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(x[8 * j + k]);
+                    const int dim = dim_of<D>(at + j);
+                    if (lone && there) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const __nv_bfloat162 h = __floats2bfloat162_rn(y[2 * k] * r * f1 * f2, y[2 * k + 1] * r * f1 * f2);
+                            w[k] = *reinterpret_cast<const uint32_t*>(&h);
                         }
+                        *reinterpret_cast<uint4*>(o + dim) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
-                    __syncwarp();
+                    if (!lone) {
+                        *reinterpret_cast<float4*>(part + dim) = make_float4(y[0], y[1], y[2], y[3]);
+                        *reinterpret_cast<float4*>(part + dim + 4) = make_float4(y[4], y[5], y[6], y[7]);
+                    }
                 }
-            } else {
-                // parts of a tile lie one behind the other from 2 x its first CTA + 1 on (as in fa_q8_attn.cu)
-                const unsigned cta0 = g.u / line.per;
-                float* o = a.part + ((size_t)(cta0 + 1 + blockIdx.x) * kRows + tile * 128 + row) * (D + 4);
-#pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    float x[32];
-                    tmem_ld32(to + c, x);
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(o + c + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
-                }
-                *reinterpret_cast<float4*>(o + D) = make_float4(m, mp, l0, 0.f);
+                __syncwarp();
             }
+            if (!lone && half == 0) *reinterpret_cast<float4*>(part + D) = make_float4(m, mp, l0, 0.f);
             fence_before();                                // the next segment's MMAs come behind its first p_full
         }
-    } else if (warp < kMma) {
+    } else if (warp != kMma) {
         // ---- 8-bit values to halves ----
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConv));
-        constexpr int kChunks = D / 16, kPass = 128 / kChunks, kPasses = kTok / kPass;       // 16-value chunks of a row; rows of a pass
-        const int t = tid - kConv * 32, ch = t % kChunks, r0 = t / kChunks;
-        uint4 raw[kPasses];                                // of the step that comes: K of a block, then V
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
+        constexpr int kChunks = D / 16, kRowsOf = 32 / kChunks, kItems = kTok / kRowsOf;      // 16-value chunks of a row; rows of a warp's load; loads of a side
+        constexpr int kMine = (kItems + kConvWarps - 1) / kConvWarps;                         // ... of a warp
+        const int w0 = warp < kMma ? warp - kConv : warp - kConv - 1, ch = lane % kChunks, r0 = lane / kChunks;
+        uint4 raw[kMine];                                  // of the step that comes: K of a block, then V
         const unsigned char* tails[2] = {static_cast<const unsigned char*>(a.c.k_tail), static_cast<const unsigned char*>(a.c.v_tail)};
         auto paged_of = [&](const Seg& g) { return g.len >> s.lb << s.lb; };
         // Lanes 0-7: where 16 tokens of block i lie each, counted in 16 rows of the pages; kGone where no page is, kTail in the tail and
@@ -451,10 +479,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
             if (page < 0 || page >= s.n_pages) return kGone;
             return (uint32_t)((((size_t)page * s.H + g.h) * (size_t)s.blk + (tok & (s.blk - 1))) >> 4);
         };
-        auto scales_of = [&](const Seg& g, int i, uint32_t at) {
+        auto scales_of = [&](const Seg& g, int i, uint32_t at) {     // K's and V's
             const size_t ph = at >> (s.lb - 4);
-            float2 k = make_float2(ld_if(a.c.k_scale + ph, at < kTail), ld_if(a.c.v_scale + ph, at < kTail));
-            if (at == kGone) k.y = -1.f;
+            float2 k = make_float2(0.f, 0.f);
+            if (at < kTail) k = make_float2(__ldg(a.c.k_scale + ph), __ldg(a.c.v_scale + ph));
             if (at == kTail && i * kTok + 16 * (lane & 7) < g.len) {
                 const float* am = a.c.tail_amax + ((size_t)g.b * s.H + g.h) * 2;
                 const uint32_t km = __float_as_uint(am[0]), vm = __float_as_uint(am[1]);
@@ -463,98 +491,118 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
             }
             return k;
         };
-        const uint32_t lane_at = (uint32_t)((r0 & 15) * D + 16 * ch);
-        auto in_pages = [&](const Seg& g, int i) { return (i + 1) * kTok <= paged_of(g); };      // the block, as a whole (others are read when they are converted)
-        auto fetch = [&](int p, const uint8_t* side, uint32_t pages, bool there) {
-            const uint32_t at = __shfl_sync(0xffffffffu, pages, (p * kPass + r0) >> 4);
-            raw[p] = ld_if16(side + (size_t)at * (16 * D) + lane_at, there && at < kTail);
+        // A block that lies in pages as a whole is loaded a step ahead; others are read when they are converted.
+        auto in_pages = [&](uint32_t pages) { return !__any_sync(0xffffffffu, pages >= kTail); };
+        auto fetch = [&](int p, const uint8_t* side, uint32_t pages) {
+            const int it = w0 + p * kConvWarps;
+            if (it < kItems) {                             // (the whole warp)
+                const int r = it * kRowsOf + r0;
+                const uint32_t at = __shfl_sync(0xffffffffu, pages, r >> 4);
+                raw[p] = __ldg(reinterpret_cast<const uint4*>(side + (size_t)at * (16 * D) + (uint32_t)((r & 15) * D + 16 * ch)));
+            }
         };
-        // (the upper half of the lanes of a row stores its second chunk first: no two meet in a bank)
-        const bool swap = kChunks == 8 && ch >= 4;
         auto put = [&](unsigned char* dst, int r, const uint32_t (&h)[8]) {
-            const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
-            *reinterpret_cast<uint4*>(dst + operand_offset(r, 2 * ch + (swap ? 1 : 0))) = swap ? hi : lo;
-            *reinterpret_cast<uint4*>(dst + operand_offset(r, 2 * ch + (swap ? 0 : 1))) = swap ? lo : hi;
+            *reinterpret_cast<uint4*>(dst + operand_offset<D>(r, 2 * ch)) = make_uint4(h[0], h[1], h[2], h[3]);
+            *reinterpret_cast<uint4*>(dst + operand_offset<D>(r, 2 * ch + 1)) = make_uint4(h[4], h[5], h[6], h[7]);
         };
-        auto halves = [&](const uint4& x, uint32_t (&h)[8]) {
+        auto halves = [&](const uint4& x, bool low, uint32_t (&h)[8]) {           // low: q + 128 as the last bits
             const uint32_t w[4] = {q8_flip<FMT>(x.x), q8_flip<FMT>(x.y), q8_flip<FMT>(x.z), q8_flip<FMT>(x.w)};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                h[2 * k] = q8_halves<FMT>(w[k], 0);
-                h[2 * k + 1] = q8_halves<FMT>(w[k], 1);
+                if (FMT == FA_Q8_INT8 && low) {
+                    h[2 * k] = __byte_perm(w[k], 0u, 0x4140);
+                    h[2 * k + 1] = __byte_perm(w[k], 0u, 0x4342);
+                } else {
+                    h[2 * k] = q8_halves<FMT>(w[k], 0);
+                    h[2 * k + 1] = q8_halves<FMT>(w[k], 1);
+                }
             }
         };
         bool more = line.next(a, g);
         uint32_t pages = kTail;
         float2 scale = make_float2(0.f, 0.f);
+        bool inside = false;
         if (more) {
             pages = pages_of(g, g.i0);
             scale = scales_of(g, g.i0, pages);
+            inside = in_pages(pages);
+            if (inside)
 #pragma unroll
-            for (int p = 0; p < kPasses; ++p) fetch(p, a.c.k_pages, pages, in_pages(g, g.i0));
+                for (int p = 0; p < kMine; ++p) fetch(p, a.c.k_pages, pages);
         }
         while (ok && more) {
             Seg nx = g;
             for (int i = g.i0; i < g.i1; ++i, ++blk) {
                 const uint32_t st = blk & 1, ph = (blk >> 1) & 1;
-                const bool inside = in_pages(g, i);
                 if (i + 1 == g.i1) more = line.next(a, nx);
-                const bool go = i + 1 < g.i1 || more;
                 const int ni = i + 1 < g.i1 ? i + 1 : nx.i0;                // (nx is g within the segment)
-                const uint32_t npages = go ? pages_of(nx, ni) : kTail;
-                const bool ninside = go && in_pages(nx, ni);
+                const uint32_t npages = i + 1 < g.i1 || more ? pages_of(nx, ni) : kTail;
+                const bool ninside = in_pages(npages);
                 float2 nscale = make_float2(0.f, 0.f);
 #pragma unroll 1
                 for (int side = 0; side < 2; ++side) {
                     if (blk >= 2) ok = mbar_wait((side ? bar.v_empty : bar.k_empty) + st, ph ^ 1, &fail, status);
                     if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                    if (side == 0 && warp == kConv) {
-                        const unsigned gone = __ballot_sync(0xffffffffu, pages == kGone);
-                        if (lane < 8) sc[blk % kScSlots][lane] = scale;
-                        if (lane == 0) {
-                            sc_gone[blk % kScSlots] = gone != 0;
-                            if (gone) q8_report(status, FA_ERR_INDEX);
+                    if (side == 0) {
+                        if (warp == kConv) {
+                            const unsigned gone = __ballot_sync(0xffffffffu, pages == kGone) & 0xffu, tail = __ballot_sync(0xffffffffu, pages == kTail) & 0xffu;
+                            if (lane < 8) sc[blk % kScSlots][lane] = make_float2(scale.y != scale.y ? scale.y : scale.x, log2f(scale.y));
+                            if (lane == 0) {
+                                sc_marks[blk % kScSlots] = (int)(gone | tail << 8);
+                                if (gone) q8_report(status, FA_ERR_INDEX);
+                            }
                         }
+                        if (i + 1 < g.i1 || more) nscale = scales_of(nx, ni, npages);
                     }
-                    if (side == 0) nscale = scales_of(nx, ni, go ? npages : kGone);
                     unsigned char* dst = (side ? vs : ks) + st * kTile;
                     const uint8_t* next_side = side ? a.c.k_pages : a.c.v_pages;
                     const uint32_t next_pages = side ? npages : pages;
                     const bool next_inside = side ? ninside : inside;
-                    if (inside) {
+                    if (inside && next_inside) {
 #pragma unroll
-                        for (int p = 0; p < kPasses; ++p) {
+                        for (int p = 0; p < kMine; ++p) {
                             uint32_t h[8];
-                            halves(raw[p], h);
-                            fetch(p, next_side, next_pages, next_inside);
-                            put(dst, p * kPass + r0, h);
+                            halves(raw[p], side == 0, h);
+                            fetch(p, next_side, next_pages);
+                            if (w0 + p * kConvWarps < kItems) put(dst, (w0 + p * kConvWarps) * kRowsOf + r0, h);
                         }
                     } else {
-#pragma unroll 1
-                        for (int p = 0; p < kPasses; ++p) {
-                            const int r = p * kPass + r0, tok = i * kTok + r;
-                            const uint32_t at = __shfl_sync(0xffffffffu, pages, r >> 4);
-                            uint32_t h[8];
-                            if (at == kTail && tok < g.len) {      // the tail: scaled by the power of two above its largest magnitude
-                                const uint32_t mx = __float_as_uint(a.c.tail_amax[((size_t)g.b * s.H + g.h) * 2 + side]);
-                                Vec16<__nv_bfloat16> v;
-                                if (mx < 0x7f800000u)
-                                    v.load(reinterpret_cast<const __nv_bfloat16*>(tails[side]) +
-                                           (((size_t)g.b * s.H + g.h) * (size_t)s.blk + (tok - paged_of(g))) * D + 16 * ch);
-                                else v.zero();
-                                const float f = pow2i(13 - max((int)(mx >> 23) - 127, -100));
+                        if (inside) {                      // its last step: nothing to be loaded ahead
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) h[k] = half2_of(v.at(2 * k) * f, v.at(2 * k + 1) * f);
-                            } else if (at < kTail) {
-                                halves(ld_if16((side ? a.c.v_pages : a.c.k_pages) + (size_t)at * (16 * D) + lane_at, true), h);
-                            } else {
-#pragma unroll
-                                for (int k = 0; k < 8; ++k) h[k] = 0u;
+                            for (int p = 0; p < kMine; ++p) {
+                                uint32_t h[8];
+                                halves(raw[p], side == 0, h);
+                                if (w0 + p * kConvWarps < kItems) put(dst, (w0 + p * kConvWarps) * kRowsOf + r0, h);
                             }
-                            put(dst, r, h);
-                        }
+                        } else {
+#pragma unroll 1
+                            for (int it = w0; it < kItems; it += kConvWarps) {
+                                const int r = it * kRowsOf + r0, tok = i * kTok + r;
+                                const uint32_t at = __shfl_sync(0xffffffffu, pages, r >> 4);
+                                uint32_t h[8];
+                                if (at == kTail && tok < g.len) {  // the tail: scaled by the power of two above its largest magnitude
+                                    const uint32_t mx = __float_as_uint(a.c.tail_amax[((size_t)g.b * s.H + g.h) * 2 + side]);
+                                    Vec16<__nv_bfloat16> v;
+                                    if (mx < 0x7f800000u)
+                                        v.load(reinterpret_cast<const __nv_bfloat16*>(tails[side]) +
+                                               (((size_t)g.b * s.H + g.h) * (size_t)s.blk + (tok - paged_of(g))) * D + 16 * ch);
+                                    else v.zero();
+                                    const float f = pow2i(13 - max((int)(mx >> 23) - 127, -100));
 #pragma unroll
-                        for (int p = 0; p < kPasses; ++p) fetch(p, next_side, next_pages, next_inside);
+                                    for (int k = 0; k < 8; ++k) h[k] = half2_of(v.at(2 * k) * f, v.at(2 * k + 1) * f);
+                                } else if (at < kTail) {
+                                    halves(__ldg(reinterpret_cast<const uint4*>((side ? a.c.v_pages : a.c.k_pages) + (size_t)at * (16 * D) + (uint32_t)((r & 15) * D + 16 * ch))),
+                                           side == 0, h);
+                                } else {
+#pragma unroll
+                                    for (int k = 0; k < 8; ++k) h[k] = 0u;
+                                }
+                                put(dst, r, h);
+                            }
+                        }
+                        if (next_inside)
+#pragma unroll
+                            for (int p = 0; p < kMine; ++p) fetch(p, next_side, next_pages);
                     }
                     fence_smem();
                     __syncwarp();
@@ -563,17 +611,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                 if (!ok) break;
                 pages = npages;
                 scale = nscale;
+                inside = ninside;
             }
             g = nx;
         }
     } else {
         // ---- the MMAs ----
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsMma));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
         // operands: K-major with 64 dims to a row of 128 bytes, the next 64 a box further; V the same read along the tokens (MN-major)
         const uint64_t qd0 = umma_desc(smem_u32(qs), 1, 1024 >> 4), kd0 = umma_desc(smem_u32(ks), 1, 1024 >> 4);
         const uint64_t vd0 = umma_desc(smem_u32(vs), (kTok * 128) >> 4, 1024 >> 4);
         uint32_t n_p[2] = {0, 0}, n_q[2] = {0, 0};         // phases of p_full, q_full
-        while (warp == kMma && ok && line.next(a, g)) {
+        while (ok && line.next(a, g)) {
             const int tiles = two_tiles(g) ? 2 : 1;
             const int n = g.i1 - g.i0;
             for (int t = 0; t < tiles && ok; ++t) ok = mbar_wait(bar.q_full + t, n_q[t]++ & 1, &fail, status);
@@ -592,7 +641,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                         if (lane == 0) {
                             const uint32_t p = tmem + 128 * t, o = tmem + 256 + D * t;
 #pragma unroll
-                            for (int k = 0; k < kTok / 16; ++k) umma_ts(o, p + 8 * k, vd + (uint64_t)(k * 2048 >> 4), kIdescO, i > 1 || k > 0);
+                            for (int k = 0; k < kTok / 16; ++k) umma_ts(o, p + 8 * k + 32 * (k >> 2), vd + (uint64_t)(k * 2048 >> 4), kIdescO, i > 1 || k > 0);
                             if (i == n) umma_commit(bar.o_done + t);
                         }
                         __syncwarp();
