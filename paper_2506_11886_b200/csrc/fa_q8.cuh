@@ -77,52 +77,95 @@ __device__ __forceinline__ void q8_report(int32_t* status, int err) { atomicCAS(
 // an ulp or two; the remainder x * top - y * amax is exact (x * top and the products have few bits), and y + remainder / amax
 // rounds to the nearest number, which is the quotient itself where that is representable, as half-way points are.
 // Elsewhere the quotient is further from a half-way point than the rounding: 2 x top and (an odd number) x amax are whole multiples of one unit, so
-// 2^-16 relative for 8-bit significands and 2^-32 for 24 (in 64 bits).  p is a power of two that keeps all of it normal; values below 2^-60 amax become zero either way.
+// 2^-16 relative for 8-bit significands and 2^-32 for 24 (in 64 bits).  p, a power of two, keeps all of it normal; values below 2^-60 amax become zero either way.
 template <typename T>
 struct Q8Real { using type = float; };
 template <>
 struct Q8Real<float> { using type = double; };
 
+// Two of them as one operand of the packed fp32 instructions; of 64 bits, two.
+template <typename R>
+struct Q8Two;
+template <>
+struct Q8Two<float> {
+    unsigned long long v;
+    static __device__ __forceinline__ Q8Two of(float a, float b) {
+        Q8Two r;
+        asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+        return r;
+    }
+    __device__ __forceinline__ Q8Two times(Q8Two b) const {
+        Q8Two r;
+        asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(v), "l"(b.v));
+        return r;
+    }
+    __device__ __forceinline__ Q8Two times_plus(Q8Two b, Q8Two c) const {
+        Q8Two r;
+        asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(v), "l"(b.v), "l"(c.v));
+        return r;
+    }
+    __device__ __forceinline__ Q8Two plus(Q8Two b) const {
+        Q8Two r;
+        asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(v), "l"(b.v));
+        return r;
+    }
+    __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+template <>
+struct Q8Two<double> {
+    double a, b;
+    static __device__ __forceinline__ Q8Two of(double x, double y) { return {x, y}; }
+    __device__ __forceinline__ Q8Two times(Q8Two o) const { return {a * o.a, b * o.b}; }
+    __device__ __forceinline__ Q8Two times_plus(Q8Two o, Q8Two c) const { return {fma(a, o.a, c.a), fma(b, o.b, c.b)}; }
+    __device__ __forceinline__ Q8Two plus(Q8Two o) const { return {a + o.a, b + o.b}; }
+    __device__ __forceinline__ void get(double& x, double& y) const { x = a; y = b; }
+};
+
 template <int FMT, typename T>
 struct Q8Round {
     using R = typename Q8Real<T>::type;
+    using Two = Q8Two<R>;
     static constexpr float kTop = FMT == FA_Q8_INT8 ? 127.f : 448.f;
-    R amax, inv;
-    float p;
+    R top, minus, inv;               // p top, -p amax, 1 / (p amax)
     bool live;                       // some value is not zero, all are finite
     __device__ __forceinline__ explicit Q8Round(uint32_t amax_bits) {
-        const float a = __uint_as_float(amax_bits);
         live = amax_bits != 0 && amax_bits < 0x7f800000u;
-        p = amax_bits < 0x21800000u ? 0x1p64f : amax_bits > 0x5d800000u ? 0x1p-64f : 1.f;
-        const float as = a * p;
-        amax = (R)as;
-        inv = live ? (R)1 / amax : (R)0;
+        const float p = amax_bits < 0x21800000u ? 0x1p64f : amax_bits > 0x5d800000u ? 0x1p-64f : 1.f;
+        const float as = __uint_as_float(amax_bits) * p;
+        top = (R)(kTop * p);
+        minus = (R)-as;
+        inv = live ? (R)1 / (R)as : (R)0;
     }
-    __device__ __forceinline__ R quotient(float x) const {
-        const R xt = (R)(x * p) * (R)kTop;
-        const R y = xt * inv;
-        return fma(fma(-y, amax, xt), inv, y);
+    __device__ __forceinline__ Two quotient(float x0, float x1) const {
+        const Two i2 = Two::of(inv, inv);
+        const Two xt = Two::of((R)x0, (R)x1).times(Two::of(top, top)), y = xt.times(i2);
+        return y.times_plus(Two::of(minus, minus), xt).times_plus(i2, y);
     }
     // Four values to four bytes.
     __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d) const {
         if (!live) return 0u;
+        Two q0 = quotient(a, b), q1 = quotient(c, d);
+        R r0, r1, r2, r3;
         uint32_t r;
         if constexpr (FMT == FA_Q8_INT8) {
-            int i0, i1, i2, i3;
-            if constexpr (sizeof(R) == 8) {
-                i0 = __double2int_rn(quotient(a)); i1 = __double2int_rn(quotient(b)); i2 = __double2int_rn(quotient(c)); i3 = __double2int_rn(quotient(d));
-            } else {
-                i0 = __float2int_rn(quotient(a)); i1 = __float2int_rn(quotient(b)); i2 = __float2int_rn(quotient(c)); i3 = __float2int_rn(quotient(d));
-            }
-            r = (uint32_t)(i0 & 255) | ((uint32_t)(i1 & 255) << 8) | ((uint32_t)(i2 & 255) << 16) | ((uint32_t)i3 << 24);
+            // 1.5 2^23 (2^52) behind it, a sum's last bits are the quotient rounded to a whole number, half to even
+            constexpr R kBehind = sizeof(R) == 8 ? (R)6755399441055744.0 : (R)12582912.0f;
+            q0 = q0.plus(Two::of(kBehind, kBehind));
+            q1 = q1.plus(Two::of(kBehind, kBehind));
+            q0.get(r0, r1);
+            q1.get(r2, r3);
+            r = __byte_perm(__byte_perm(last_word(r0), last_word(r1), 0x0040), __byte_perm(last_word(r2), last_word(r3), 0x0040), 0x5410);
         } else {
-            const float f0 = narrow(quotient(a)), f1 = narrow(quotient(b)), f2 = narrow(quotient(c)), f3 = narrow(quotient(d));
+            q0.get(r0, r1);
+            q1.get(r2, r3);
             asm("{\n .reg .b16 lo, hi;\n cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n mov.b32 %0, {lo, hi};\n}\n"
                 : "=r"(r)
-                : "f"(f0), "f"(f1), "f"(f2), "f"(f3));
+                : "f"(narrow(r0)), "f"(narrow(r1)), "f"(narrow(r2)), "f"(narrow(r3)));
         }
         return r;
     }
+    static __device__ __forceinline__ uint32_t last_word(float x) { return __float_as_uint(x); }
+    static __device__ __forceinline__ uint32_t last_word(double x) { return (uint32_t)__double2loint(x); }
     // 64 to 32 bits by rounding to odd: the second rounding, to 4 bits, then comes out as one from 64 bits would.
     static __device__ __forceinline__ float narrow(float y) { return y; }
     static __device__ __forceinline__ float narrow(double y) {

@@ -37,8 +37,8 @@ fa_status check_tokens(const fa_q8_layout* l, const void* K, const void* V, int6
     if (n == 0) return FA_OK;
     if (!K || !V || !aligned16(K) || !aligned16(V)) return FA_ERR_INVALID_ARG;
     if (sb < 0 || st < l->head_dim || sh < l->head_dim || ((sb | st | sh) & 7)) return FA_ERR_INVALID_ARG;
-    // blocks and heads of a launch in one grid dimension
-    if (((int64_t)n / l->block + 2) * 2 * l->n_kv_heads > 0x7fffffff) return FA_ERR_UNSUPPORTED;
+    // blocks (of 16 tokens at least) and heads of a launch are counted in 32 bits
+    if (((int64_t)n / 16 + 2) * 2 * l->n_kv_heads > 0x7fffffff) return FA_ERR_UNSUPPORTED;
     return FA_OK;
 }
 

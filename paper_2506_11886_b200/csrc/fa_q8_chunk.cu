@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
     }
 }
 
-// Joins the parts of tiles that were cut, in the order of the tokens; zeros for tiles that see nothing.  A CTA takes 32 rows of a tile.
+// Joins the parts of tiles that were cut, in the order of the tokens; zeros for tiles that see nothing.  A warp takes a row.
 template <int D>
 __global__ void __launch_bounds__(256) q8_chunk_join_kernel(const ChunkArgs a) {
     const Q8Dims& s = a.s;
@@ -699,14 +699,14 @@ __global__ void __launch_bounds__(256) q8_chunk_join_kernel(const ChunkArgs a) {
         if (parts == 1) return;
     }
     constexpr int kPitch = D + 4, kVec = D / 32;           // floats of a lane
-    for (int r = blockIdx.y * 32 + warp; r < (int)blockIdx.y * 32 + 32; r += 8) {
-        const int col = ct * kRows + r, qi = col / s.G;
+    {
+        const int r = (int)blockIdx.y * 8 + warp, col = ct * kRows + r, qi = col / s.G;
         if (qi >= a.n_q) return;
         const float* p = a.part + ((size_t)(2 * cta0 + 1) * kRows + r) * kPitch;
         float m = kNegBig, mp = kNegBig, l = 0.f, o[kVec];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) o[i] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
         for (unsigned j = 0; j < parts; ++j) {
             const float* pj = p + (size_t)j * kRows * kPitch;
             const float4 hd = __ldcg(reinterpret_cast<const float4*>(pj + D));
@@ -737,14 +737,16 @@ cudaError_t chunk_of(const ChunkArgs& a, cudaStream_t stream) {
     const size_t smem = (size_t)6 * kTok * D * 2 + 1024;
     cudaError_t e = ensure_dynamic_smem(q8_chunk_kernel<FMT, D>, smem);
     if (e == cudaSuccess) e = launch_behind(q8_chunk_kernel<FMT, D>, dim3((unsigned)a.ctas), kChunkThreads, smem, stream, a);
-    if (e == cudaSuccess) e = launch_behind(q8_chunk_join_kernel<D>, dim3((unsigned)(a.s.B * a.n_ct * a.s.H), kRows / 32), 256, 0, stream, a);
+    if (e == cudaSuccess) e = launch_behind(q8_chunk_join_kernel<D>, dim3((unsigned)(a.s.B * a.n_ct * a.s.H), kRows / 8), 256, 0, stream, a);
     return e;
 }
 
 }  // namespace
 
 bool q8_chunk_takes(const Q8Dims& s, int dtype, int n_q) {
-    if (dtype != FA_BF16 || s.d > 128 || (long long)n_q * s.G < 64) return false;
+    // Over 64 columns to a KV head: one row of 16384 tokens, 32/8 heads of 128, us here / by tiles of 16 columns: 64 columns 55 / 49, 128 56 / 86,
+    // 256 68 / 155; of 1000 tokens 128 columns 24 / 17, 512 30 / 40; eight rows of 4000 tokens 64 columns 68 / 87.
+    if (dtype != FA_BF16 || s.d > 128 || (long long)n_q * s.G <= 64) return false;
     const long long tiles = (long long)s.B * chunk_tiles(s, n_q);
     return tiles * s.H * (((long long)s.nb * s.blk + kTok - 1) / kTok) <= 0x7fffffff && tiles * s.H <= 0x7fffffff;
 }

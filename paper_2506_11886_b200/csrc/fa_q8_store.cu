@@ -1,15 +1,19 @@
 // fa_q8_write, fa_q8_append, fa_q8_read: tokens into the dense cache in 8 bits and back.
 //
-// A CTA owns one block of one KV head and side (K or V).  A block that the call completes is rounded: its tokens, those
-// that the tail holds already and the new ones, go to registers once, the CTA finds their largest magnitude, and 16 bytes
+// A group of threads takes one block of one KV head and side (K or V) at a time, 32 values or more to a thread.  A block that the call
+// completes is rounded: its tokens, those that the tail holds already and the new ones, go to registers once, the group finds their largest magnitude, and 16 bytes
 // a thread leave as a page.  The block that stays incomplete is copied to the tail, with the running largest magnitude.  The
 // first block of a row that has a tail is read from it, and the last one of the call written to it: where these are
-// two blocks, one CTA does both in that order.  The last CTA to take the ticket sets the rows' lengths, which the others have read by then.
+// two blocks, one group does both in that order.  Appending, each CTA takes a ticket once it has read the rows' lengths; the last one sets them.
 // Bound by HBM: 2 (or 4) bytes in and 1 out per value, whole sectors on both sides.
+#include <type_traits>
+
 #include "fa_q8.cuh"
 
 namespace fa {
 namespace {
+
+constexpr int kStoreThreads = 256;
 
 template <typename T>
 struct StoreArgs {
@@ -19,213 +23,254 @@ struct StoreArgs {
     int64_t sb, st, sh;
     int n;
     const int32_t* n_row;
-    int append;
+    int append, touched;             // blocks of a row that the call can touch
+    int ld;                          // log2 of the head dim
 };
 
-template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(1024, 1) q8_store_kernel(const StoreArgs<T> a) {
-    const Q8Dims& s = a.s;
-    __shared__ uint32_t red[32];
-    __shared__ int bad_s;
-    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5;
-    const int h2 = (int)(blockIdx.x % (unsigned)(2 * s.H)), x = (int)(blockIdx.x / (unsigned)(2 * s.H)), b = blockIdx.y;
-    const int h = h2 >> 1, side = h2 & 1;
-    const int held = a.append ? a.c.state[b * kQ8State] : 0;
-    const int cap = s.nb << s.lb;
+// What the call does to row b.
+struct StoreRow {
+    int held, total, first, whole;   // tokens before and after; the first block that gets tokens, complete blocks after
+    bool goes;                       // there are new tokens and they fit
+};
+template <typename T>
+__device__ __forceinline__ StoreRow store_row(const StoreArgs<T>& a, int b, int held) {
+    const int cap = a.s.nb << a.s.lb;
     int n = a.n_row ? a.n_row[b] : a.n;
     n = n < 0 ? 0 : n > a.n ? a.n : n;
-    const bool fits = held >= 0 && held <= cap && n <= cap - held;
-    const int total = held + n;
-    const int first = held >> s.lb, r = held & (s.blk - 1);          // the first block that gets tokens, what the tail has of it
-    const int whole = total >> s.lb;                                 // complete blocks behind the call
-    const int blk = first + x;
-    const int32_t* table = a.c.table + (size_t)b * s.nb;
-
-    const bool two = r > 0 && whole > first;                         // the tail is read and written
-    const bool completes = fits && n > 0 && blk < whole;
-    const bool fills = fits && n > 0 && (total & (s.blk - 1)) != 0 && (two ? x == 0 : blk == whole);
-    if (tid == 0) bad_s = !fits;
-    __syncthreads();
-    if (fills) {                                                     // the tail stays as it is if any block of the row has no page
-        for (int i = first + tid; i < whole; i += nt) {
-            const int page = table[i];
-            if (page < 0 || page >= s.n_pages) bad_s = 1;
-        }
+    StoreRow r;
+    r.held = held;
+    r.goes = held >= 0 && held <= cap && n <= cap - held && n > 0;
+    r.total = r.goes ? held + n : held;
+    r.first = held >> a.s.lb;
+    r.whole = r.total >> a.s.lb;
+    return r;
+}
+// Whether every block that the call completes in row b has a page; by the threads i0, i0 + step, ...
+template <typename T>
+__device__ __forceinline__ bool pages_there(const StoreArgs<T>& a, int b, const StoreRow& r, int i0, int step) {
+    bool ok = true;
+    for (int i = r.first + i0; i < r.whole; i += step) {
+        const int page = a.c.table[(size_t)b * a.s.nb + i];
+        ok = ok && page >= 0 && page < a.s.n_pages;
     }
+    return ok;
+}
 
-    T* tail = reinterpret_cast<T*>(side ? a.c.v_tail : a.c.k_tail) + ((size_t)b * s.H + h) * (size_t)s.blk * D;
-    const T* src = (side ? a.V : a.K) + (int64_t)b * a.sb + (int64_t)h * a.sh;
-    float* amax_out = a.c.tail_amax + ((size_t)b * s.H + h) * 2 + side;
-    const int nvec = s.blk * (D / 16);                               // two to a thread (nt = nvec / 2)
-    auto block_max = [&](uint32_t m) {
+// NV vectors of 16 values to a thread.
+template <typename T, int FMT, int NV>
+__global__ void __launch_bounds__(kStoreThreads, NV == 2 ? (sizeof(T) == 2 ? 4 : 3) : NV == 4 ? 2 : 1) q8_store_kernel(const StoreArgs<T> a) {
+    const Q8Dims& s = a.s;
+    __shared__ uint32_t red[2][kStoreThreads / 32];
+    __shared__ int held_s[32], last_s;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int lv = a.ld - 4;                                         // log2 of a row's vectors
+    const int nvec = s.blk << lv, group = nvec / NV;                 // threads of a group: whole warps
+    const int gi = tid / group, gt = tid % group, gwarps = group >> 5;
+    uint32_t turn = 0;
+    auto group_sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(1 + gi), "r"(group) : "memory"); };
+    auto group_max = [&](uint32_t m) {
         m = __reduce_max_sync(0xffffffffu, m);
-        __syncthreads();
-        if (lane == 0) red[warp] = m;
-        __syncthreads();
-        const uint32_t v = lane < (nt >> 5) ? red[lane] : 0u;
+        if (gwarps == 1) return m;
+        uint32_t* place = red[turn++ & 1];
+        if (lane == 0) place[warp] = m;
+        group_sync();
+        const uint32_t v = lane < gwarps ? place[gi * gwarps + lane] : 0u;
         return __reduce_max_sync(0xffffffffu, v);
     };
-    if (completes) {
-        const int page = table[blk];
-        const bool good = page >= 0 && page < s.n_pages;
-        if (!good && tid == 0) {
-            q8_report(a.c.status, FA_ERR_INDEX);
-            atomicExch(a.c.state + b * kQ8State + 1, 1);
+    asm volatile("griddepcontrol.launch_dependents;");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // the lengths in front of the call (of up to 32 rows at hand), then the ticket
+    if (a.append) {
+        if (tid < 32 && tid < s.B) held_s[tid] = a.c.state[tid * kQ8State];
+        if (s.B <= 32) {
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) last_s = atomicInc(reinterpret_cast<unsigned*>(a.c.status) + 1, gridDim.x - 1) == gridDim.x - 1;
         }
-        Vec16<T> v[2];
-        uint32_t m = 0;
+    }
+    __syncthreads();
+
+    const long long items = (long long)s.B * a.touched * 2 * s.H;
+    const int groups = kStoreThreads / group;
+    for (long long it = (long long)blockIdx.x * groups + gi; it < items; it += (long long)gridDim.x * groups) {
+        const unsigned per = 2u * (unsigned)s.H * (unsigned)a.touched;
+        const int b = (int)(it / per);
+        const unsigned rest = (unsigned)(it - (long long)b * per), x = rest / (2u * (unsigned)s.H), h2 = rest - x * (2u * (unsigned)s.H);
+        const int h = (int)(h2 >> 1), side = (int)(h2 & 1);
+        const StoreRow r = store_row(a, b, !a.append ? 0 : s.B <= 32 ? held_s[b] : a.c.state[b * kQ8State]);
+        if (!r.goes) continue;
+        const int blk = r.first + (int)x, k0 = r.held & (s.blk - 1);
+        const bool two = k0 > 0 && r.whole > r.first;                // the tail is read and written
+        const bool completes = blk < r.whole, fills = (r.total & (s.blk - 1)) != 0 && (two ? x == 0 : blk == r.whole);
+        if (!completes && !fills) continue;
+        const int32_t* table = a.c.table + (size_t)b * s.nb;
+        T* tail = reinterpret_cast<T*>(side ? a.c.v_tail : a.c.k_tail) + (((size_t)b * s.H + h) * (size_t)s.blk << a.ld);
+        const T* src = (side ? a.V : a.K) + (int64_t)b * a.sb + (int64_t)h * a.sh;
+        if (completes) {
+            const int page = table[blk];
+            const bool good = page >= 0 && page < s.n_pages;
+            if (!good && gt == 0) q8_report(a.c.status, FA_ERR_INDEX);
+            Vec16<T> v[NV];
+            uint32_t m = 0;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int i = tid + k * nt, t = i / (D / 16), e = (i % (D / 16)) * 16;
-            const int at = (blk << s.lb) + t;                        // the token's place in the row
-            if (i < nvec) v[k].load(at < held ? tail + (size_t)t * D + e : src + (int64_t)(at - held) * a.st + e);
-            else v[k].zero();
-            m = max(m, v[k].amax_bits());
-        }
-        m = block_max(m);
-        if (good) {
-            const Q8Round<FMT, T> to(m);
-            const size_t ph = (size_t)page * s.H + h;
-            uint8_t* out = (side ? a.c.v_pages : a.c.k_pages) + ph * (size_t)(s.blk * D);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int i = tid + k * nt;
-                if (i >= nvec) break;
-                uint4 o;
-                o.x = to.pack(v[k].at(0), v[k].at(1), v[k].at(2), v[k].at(3));
-                o.y = to.pack(v[k].at(4), v[k].at(5), v[k].at(6), v[k].at(7));
-                o.z = to.pack(v[k].at(8), v[k].at(9), v[k].at(10), v[k].at(11));
-                o.w = to.pack(v[k].at(12), v[k].at(13), v[k].at(14), v[k].at(15));
-                *reinterpret_cast<uint4*>(out + (size_t)i * 16) = o;
+            for (int k = 0; k < NV; ++k) {
+                const int i = gt + k * group, t = i >> lv, e = (i & ((1 << lv) - 1)) << 4;
+                const int at = (blk << s.lb) + t;                    // the token's place in the row
+                v[k].load(at < r.held ? tail + ((size_t)t << a.ld) + e : src + (int64_t)(at - r.held) * a.st + e);
             }
-            if (tid == 0) (side ? a.c.v_scale : a.c.k_scale)[ph] = Q8Round<FMT, T>::scale(m);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) m = max(m, v[k].amax_bits());
+            m = group_max(m);
+            if (good) {
+                const Q8Round<FMT, T> to(m);
+                const size_t ph = (size_t)page * s.H + h;
+                uint8_t* out = (side ? a.c.v_pages : a.c.k_pages) + (ph * (size_t)s.blk << a.ld);
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    uint4 o;
+                    o.x = to.pack(v[k].at(0), v[k].at(1), v[k].at(2), v[k].at(3));
+                    o.y = to.pack(v[k].at(4), v[k].at(5), v[k].at(6), v[k].at(7));
+                    o.z = to.pack(v[k].at(8), v[k].at(9), v[k].at(10), v[k].at(11));
+                    o.w = to.pack(v[k].at(12), v[k].at(13), v[k].at(14), v[k].at(15));
+                    *reinterpret_cast<uint4*>(out + (size_t)(gt + k * group) * 16) = o;
+                }
+                if (gt == 0) (side ? a.c.v_scale : a.c.k_scale)[ph] = Q8Round<FMT, T>::scale(m);
+            }
+        }
+        if (fills) {
+            // the tail stays as it is if any block of the row has no page; the group decides as one
+            if (group_max(pages_there(a, b, r, gt, group) ? 0u : 1u)) continue;
+            // the row's new tokens from t0 on, behind the n0 that the tail has of this block
+            const int t0 = max(r.held, r.whole << s.lb), n0 = r.whole > r.first ? 0 : k0;
+            const int nv = (r.total - t0) << lv;
+            uint32_t m = 0;
+            for (int i = gt; i < nv; i += group) {
+                const int t = i >> lv, e = (i & ((1 << lv) - 1)) << 4;
+                Vec16<T> v;
+                v.load(src + (int64_t)(t0 - r.held + t) * a.st + e);
+                v.store(tail + ((size_t)(n0 + t) << a.ld) + e);
+                m = max(m, v.amax_bits());
+            }
+            m = group_max(m);
+            if (gt == 0) {
+                float* amax = a.c.tail_amax + ((size_t)b * s.H + h) * 2 + side;
+                const float before = n0 > 0 ? *amax : 0.f;
+                *amax = __uint_as_float(max(m, __float_as_uint(before)));
+            }
         }
     }
-    __syncthreads();
-    if (fills && !bad_s) {
-        // the row's new tokens from t0 on, behind the k0 that the tail has of this block
-        const int t0 = max(held, whole << s.lb), k0 = whole > first ? 0 : r;
-        const int nv = (total - t0) * (D / 16);
-        uint32_t m = 0;
-        for (int i = tid; i < nv; i += nt) {
-            const int t = i / (D / 16), e = (i % (D / 16)) * 16;
-            Vec16<T> v;
-            v.load(src + (int64_t)(t0 - held + t) * a.st + e);
-            v.store(tail + (size_t)(k0 + t) * D + e);
-            m = max(m, v.amax_bits());
-        }
-        m = block_max(m);
-        if (tid == 0) {
-            const float before = k0 > 0 ? *amax_out : 0.f;
-            *amax_out = __uint_as_float(max(m, __float_as_uint(before)));
-        }
-    }
-    // the ticket
-    __shared__ int last_s;
-    __syncthreads();
-    if (tid == 0) {
+    // ---- the rows' lengths: nobody reads them in a write ----
+    if (a.append && s.B > 32) {                                      // (the loop above has read them)
         __threadfence();
-        const unsigned all = gridDim.x * gridDim.y;
-        last_s = atomicInc(reinterpret_cast<unsigned*>(a.c.status) + 1, all - 1) == all - 1;
-        __threadfence();
+        __syncthreads();
+        if (tid == 0) last_s = atomicInc(reinterpret_cast<unsigned*>(a.c.status) + 1, gridDim.x - 1) == gridDim.x - 1;
     }
     __syncthreads();
-    if (!last_s) return;
-    for (int i = tid; i < s.B; i += nt) {
-        int32_t* st = a.c.state + i * kQ8State;
-        const int was = a.append ? st[0] : 0;
-        int add = a.n_row ? a.n_row[i] : a.n;
-        add = add < 0 ? 0 : add > a.n ? a.n : add;
-        const bool bad = atomicExch(st + 1, 0) != 0;
-        if (was < 0 || was > cap || add > cap - was) q8_report(a.c.status, FA_ERR_CAPACITY);
-        else if (!bad) st[0] = was + add;
+    if (a.append ? !last_s : blockIdx.x != gridDim.x - 1) return;
+    const int cap = s.nb << s.lb;
+    for (int b = warp; b < s.B; b += kStoreThreads / 32) {
+        int32_t* st = a.c.state + b * kQ8State;
+        const StoreRow r = store_row(a, b, a.append ? st[0] : 0);
+        const bool there = __all_sync(0xffffffffu, pages_there(a, b, r, lane, 32));
+        if (lane != 0) continue;
+        const int n = a.n_row ? a.n_row[b] : a.n;
+        if (r.held < 0 || r.held > cap || min(n, a.n) > cap - r.held) q8_report(a.c.status, FA_ERR_CAPACITY);
+        else if (there) st[0] = r.total;
         else if (!a.append) st[0] = 0;                               // (pages of its blocks may have been written)
     }
 }
 
-// A CTA reads the same tokens of one head for K and V; a thread 16 values at a time.
+// A CTA reads kReadPass x 256 pieces of one head for K and V, a piece being 16 bytes of what is written: whole lines on both sides.
+constexpr int kReadPass = 4;
 template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(256) q8_read_kernel(Q8Dims s, Q8Cache c, T* __restrict__ K, T* __restrict__ V, int64_t sb, int64_t st, int64_t sh, int t0,
                                                       int n) {
-    constexpr int kVecs = D / 16, kTok = 256 / kVecs;                // tokens that a pass of the CTA covers
+    constexpr int kE = 16 / (int)sizeof(T), kTok = 256 * kE / D;     // values of a piece; tokens that a pass of the CTA covers
+    using Bytes = typename std::conditional<kE == 8, uint2, uint32_t>::type;
+    asm volatile("griddepcontrol.launch_dependents;");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int h = (int)(blockIdx.x % (unsigned)s.H), b = blockIdx.y;
-    const int tile = (int)(blockIdx.x / (unsigned)s.H) * (2 * kTok);
+    const int t1 = t0 + (int)(blockIdx.x / (unsigned)s.H) * (kReadPass * kTok) + (int)threadIdx.x / (D / kE), e = (threadIdx.x % (D / kE)) * kE;
     const int len = c.state[b * kQ8State];
-    const int cap = s.nb << s.lb;
-    const int e = (threadIdx.x % kVecs) * 16;
-    if (len < 0 || len > cap) {
+    if (len < 0 || len > s.nb << s.lb) {
         if (threadIdx.x == 0) q8_report(c.status, FA_ERR_CAPACITY);
         return;
     }
     const int stop = min(len, t0 + n), paged = len >> s.lb << s.lb;
+    T* const out[2] = {K + (int64_t)b * sb + (int64_t)h * sh + e, V + (int64_t)b * sb + (int64_t)h * sh + e};
+    Bytes w[2][kReadPass];
+    float f[2][kReadPass];
+    bool there[kReadPass];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int t = t0 + tile + k * kTok + (int)threadIdx.x / kVecs;
-        if (t >= stop) continue;
-        const int64_t off = (int64_t)b * sb + (int64_t)(t - t0) * st + (int64_t)h * sh + e;
-        if (t >= paged) {
-            const size_t at = (((size_t)b * s.H + h) * (size_t)s.blk + (t - paged)) * D + e;
-            Vec16<T> x;
-            x.load(reinterpret_cast<const T*>(c.k_tail) + at);
-            x.store(K + off);
-            x.load(reinterpret_cast<const T*>(c.v_tail) + at);
-            x.store(V + off);
-            continue;
+    for (int p = 0; p < kReadPass; ++p) {
+        const int t = t1 + p * kTok;
+        there[p] = t < stop && t < paged;
+        if (there[p]) {
+            const int page = c.table[(size_t)b * s.nb + (t >> s.lb)];
+            if (page < 0 || page >= s.n_pages) {
+                there[p] = false;
+                q8_report(c.status, FA_ERR_INDEX);
+            } else {
+                const size_t ph = (size_t)page * s.H + h, at = (ph * (size_t)s.blk + (t & (s.blk - 1))) * D + e;
+                w[0][p] = __ldg(reinterpret_cast<const Bytes*>(c.k_pages + at));
+                w[1][p] = __ldg(reinterpret_cast<const Bytes*>(c.v_pages + at));
+                f[0][p] = __ldg(c.k_scale + ph);
+                f[1][p] = __ldg(c.v_scale + ph);
+            }
         }
-        const int page = c.table[(size_t)b * s.nb + (t >> s.lb)];
-        if (page < 0 || page >= s.n_pages) {
-            q8_report(c.status, FA_ERR_INDEX);
-            continue;
-        }
-        const size_t ph = (size_t)page * s.H + h, at = (ph * (size_t)s.blk + (t & (s.blk - 1))) * D + e;
-        const uint4 kw = *reinterpret_cast<const uint4*>(c.k_pages + at), vw = *reinterpret_cast<const uint4*>(c.v_pages + at);
-        const float ks = c.k_scale[ph], vs = c.v_scale[ph];
+    }
+#pragma unroll
+    for (int p = 0; p < kReadPass; ++p) {
+        const int t = t1 + p * kTok;
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
-            const uint4 w = side ? vw : kw;
-            const float f = side ? vs : ks;
-            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-            float x[16];
+            uint4* to = reinterpret_cast<uint4*>(out[side] + (int64_t)(t - t0) * st);
+            if (there[p]) {
+                float x[4];
+                if constexpr (kE == 8) {
+                    uint32_t o[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float y[4];
-                q8_floats<FMT>(ws[i], y);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j] * f;
-            }
-            T* out = (side ? V : K) + off;
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) *(reinterpret_cast<float4*>(out) + i) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-            } else {
-                uint32_t o[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-                    o[i] = *reinterpret_cast<const uint32_t*>(&p);
+                    for (int i = 0; i < 2; ++i) {
+                        q8_floats<FMT>(i ? w[side][p].y : w[side][p].x, x);
+                        const __nv_bfloat162 lo = __floats2bfloat162_rn(x[0] * f[side][p], x[1] * f[side][p]);
+                        const __nv_bfloat162 hi = __floats2bfloat162_rn(x[2] * f[side][p], x[3] * f[side][p]);
+                        o[2 * i] = *reinterpret_cast<const uint32_t*>(&lo);
+                        o[2 * i + 1] = *reinterpret_cast<const uint32_t*>(&hi);
+                    }
+                    *to = make_uint4(o[0], o[1], o[2], o[3]);
+                } else {
+                    q8_floats<FMT>(w[side][p], x);
+                    *reinterpret_cast<float4*>(to) = make_float4(x[0] * f[side][p], x[1] * f[side][p], x[2] * f[side][p], x[3] * f[side][p]);
                 }
-                *reinterpret_cast<uint4*>(out) = make_uint4(o[0], o[1], o[2], o[3]);
-                *(reinterpret_cast<uint4*>(out) + 1) = make_uint4(o[4], o[5], o[6], o[7]);
+            } else if (t >= paged && t < stop) {                     // the tail: as it is
+                const T* tail = reinterpret_cast<const T*>(side ? c.v_tail : c.k_tail) + (((size_t)b * s.H + h) * (size_t)s.blk + (t - paged)) * D + e;
+                *to = *reinterpret_cast<const uint4*>(tail);
             }
         }
     }
 }
 
-template <typename T, int FMT, int D>
+template <typename T, int FMT, int NV>
+cudaError_t store_launch(const StoreArgs<T>& a, cudaStream_t stream) {
+    const int groups = kStoreThreads * NV * 16 / (a.s.blk * a.s.d);
+    const long long items = (long long)a.s.B * a.touched * 2 * a.s.H, need = (items + groups - 1) / groups, most = (long long)sm_count() * 8;
+    return launch_behind(q8_store_kernel<T, FMT, NV>, dim3((unsigned)(need < most ? need : most)), kStoreThreads, 0, stream, a);
+}
+template <typename T, int FMT>
 cudaError_t store_of(const Q8Dims& s, const Q8Cache& c, const void* K, const void* V, int64_t sb, int64_t st, int64_t sh, int n, const int32_t* n_row,
                      bool append, cudaStream_t stream) {
-    const StoreArgs<T> a = {s, c, static_cast<const T*>(K), static_cast<const T*>(V), sb, st, sh, n, n_row, append};
     // blocks that n tokens can touch behind a tail of blk - 1
     const int64_t touched = n == 0 ? 1 : ((int64_t)(append ? s.blk - 1 : 0) + n - 1) / s.blk + 1;
-    q8_store_kernel<T, FMT, D><<<dim3((unsigned)(touched * 2 * s.H), (unsigned)s.B), s.blk * D / 32, 0, stream>>>(a);
-    return cudaGetLastError();
+    const StoreArgs<T> a = {s, c, static_cast<const T*>(K), static_cast<const T*>(V), sb, st, sh, n, n_row, append, (int)touched, s.d == 64 ? 6 : s.d == 128 ? 7 : 8};
+    // 32 values to a thread, so that a block of the smallest size is a warp's; 64 or 128 where it is more than 256 threads'
+    const int values = s.blk * s.d;
+    return values <= 8192 ? store_launch<T, FMT, 2>(a, stream) : values <= 16384 ? store_launch<T, FMT, 4>(a, stream) : store_launch<T, FMT, 8>(a, stream);
 }
 template <typename T, int FMT, int D>
 cudaError_t read_of(const Q8Dims& s, const Q8Cache& c, void* K, void* V, int64_t sb, int64_t st, int64_t sh, int t0, int n, cudaStream_t stream) {
-    const int tok = 2 * 256 / (D / 16);
+    const int tok = kReadPass * 256 * (16 / (int)sizeof(T)) / D;
     const int64_t tiles = ((int64_t)n + tok - 1) / tok;
-    q8_read_kernel<T, FMT, D><<<dim3((unsigned)(tiles * s.H), (unsigned)s.B), 256, 0, stream>>>(s, c, static_cast<T*>(K), static_cast<T*>(V), sb, st, sh, t0, n);
-    return cudaGetLastError();
+    return launch_behind(q8_read_kernel<T, FMT, D>, dim3((unsigned)(tiles * s.H), (unsigned)s.B), 256, 0, stream, s, c, static_cast<T*>(K), static_cast<T*>(V), sb, st, sh, t0, n);
 }
 
 #define FA_Q8_DISPATCH(CALL)                                                                                               \
@@ -247,9 +292,11 @@ cudaError_t read_of(const Q8Dims& s, const Q8Cache& c, void* K, void* V, int64_t
 
 cudaError_t launch_q8_store(const Q8Dims& s, const Q8Cache& c, int fmt, int dtype, const void* K, const void* V, int64_t sb, int64_t st, int64_t sh, int n,
                             const int32_t* n_row, bool append, cudaStream_t stream) {
-#define FA_Q8_CALL(T, F, D) store_of<T, F, D>(s, c, K, V, sb, st, sh, n, n_row, append, stream)
-    FA_Q8_DISPATCH(FA_Q8_CALL);
-#undef FA_Q8_CALL
+    if (dtype == FA_BF16)
+        return fmt == FA_Q8_INT8 ? store_of<__nv_bfloat16, FA_Q8_INT8>(s, c, K, V, sb, st, sh, n, n_row, append, stream)
+                                 : store_of<__nv_bfloat16, FA_Q8_E4M3>(s, c, K, V, sb, st, sh, n, n_row, append, stream);
+    return fmt == FA_Q8_INT8 ? store_of<float, FA_Q8_INT8>(s, c, K, V, sb, st, sh, n, n_row, append, stream)
+                             : store_of<float, FA_Q8_E4M3>(s, c, K, V, sb, st, sh, n, n_row, append, stream);
 }
 cudaError_t launch_q8_read(const Q8Dims& s, const Q8Cache& c, int fmt, int dtype, void* K, void* V, int64_t sb, int64_t st, int64_t sh, int t0, int n,
                            cudaStream_t stream) {
