@@ -1,11 +1,11 @@
 // fa_q8_write, fa_q8_append, fa_q8_read: tokens into the dense cache in 8 bits and back.
 //
-// A group of threads takes one block of one KV head and side (K or V) at a time, 32 values or more to a thread.  A block that the call
-// completes is rounded: its tokens, those that the tail holds already and the new ones, go to registers once, the group finds their largest magnitude, and 16 bytes
-// a thread leave as a page.  The block that stays incomplete is copied to the tail, with the running largest magnitude.  The
+// A group of threads takes a few blocks of one KV head and side (K or V) in turn, 32 values or more to a thread, the next block's loads under way.  A block that
+// the call completes is rounded: its tokens, those that the tail holds already and the new ones, go to registers once, the group finds their largest magnitude,
+// and 16 bytes a thread leave as a page.  The block that stays incomplete is copied to the tail, with the running largest magnitude.  The
 // first block of a row that has a tail is read from it, and the last one of the call written to it: where these are
-// two blocks, one group does both in that order.  Appending, each CTA takes a ticket once it has read the rows' lengths; the last one sets them.
-// Bound by HBM: 2 (or 4) bytes in and 1 out per value, whole sectors on both sides.
+// two blocks, one group does both in that order.  Appending, each CTA takes a ticket once it has read its row's length; the last one sets all lengths.
+// Bound by HBM and by the instructions of the rounding (about 6 a value): 2 (or 4) bytes in and 1 out per value, whole sectors on both sides.
 #include <type_traits>
 
 #include "fa_q8.cuh"
@@ -23,7 +23,7 @@ struct StoreArgs {
     int64_t sb, st, sh;
     int n;
     const int32_t* n_row;
-    int append, touched;             // blocks of a row that the call can touch
+    int append, run;                 // blocks that a group takes in turn
     int ld;                          // log2 of the head dim
 };
 
@@ -56,126 +56,126 @@ __device__ __forceinline__ bool pages_there(const StoreArgs<T>& a, int b, const 
     return ok;
 }
 
-// NV vectors of 16 values to a thread.
+// NV vectors of 16 values to a thread.  Grid: runs of `run` blocks of each group, head and side, row.
 template <typename T, int FMT, int NV>
-__global__ void __launch_bounds__(kStoreThreads, NV == 2 ? (sizeof(T) == 2 ? 4 : 3) : NV == 4 ? 2 : 1) q8_store_kernel(const StoreArgs<T> a) {
+__global__ void __launch_bounds__(kStoreThreads, NV * sizeof(T) == 4 ? 3 : NV * sizeof(T) == 8 ? 2 : 1) q8_store_kernel(const StoreArgs<T> a) {
     const Q8Dims& s = a.s;
     __shared__ uint32_t red[2][kStoreThreads / 32];
-    __shared__ int held_s[32], last_s;
+    __shared__ int last_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int lv = a.ld - 4;                                         // log2 of a row's vectors
-    const int nvec = s.blk << lv, group = nvec / NV;                 // threads of a group: whole warps
-    const int gi = tid / group, gt = tid % group, gwarps = group >> 5;
+    const int group = (s.blk << lv) / NV;                            // threads of a group: whole warps
+    const int groups = kStoreThreads / group, gi = tid / group, gt = tid % group, gwarps = group >> 5;
     uint32_t turn = 0;
-    auto group_sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(1 + gi), "r"(group) : "memory"); };
     auto group_max = [&](uint32_t m) {
         m = __reduce_max_sync(0xffffffffu, m);
         if (gwarps == 1) return m;
         uint32_t* place = red[turn++ & 1];
         if (lane == 0) place[warp] = m;
-        group_sync();
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + gi), "r"(group) : "memory");
         const uint32_t v = lane < gwarps ? place[gi * gwarps + lane] : 0u;
         return __reduce_max_sync(0xffffffffu, v);
     };
     asm volatile("griddepcontrol.launch_dependents;");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    // the lengths in front of the call (of up to 32 rows at hand), then the ticket
+    const int b = blockIdx.z, h = blockIdx.y >> 1, side = blockIdx.y & 1;
+    const int held = a.append ? a.c.state[b * kQ8State] : 0;
     if (a.append) {
-        if (tid < 32 && tid < s.B) held_s[tid] = a.c.state[tid * kQ8State];
-        if (s.B <= 32) {
+        __syncthreads();                                             // (all threads have the length)
+        if (tid == 0) {
             __threadfence();
-            __syncthreads();
-            if (tid == 0) last_s = atomicInc(reinterpret_cast<unsigned*>(a.c.status) + 1, gridDim.x - 1) == gridDim.x - 1;
+            const unsigned all = gridDim.x * gridDim.y * gridDim.z;
+            last_s = atomicInc(reinterpret_cast<unsigned*>(a.c.status) + 1, all - 1) == all - 1;
         }
     }
-    __syncthreads();
-
-    const long long items = (long long)s.B * a.touched * 2 * s.H;
-    const int groups = kStoreThreads / group;
-    for (long long it = (long long)blockIdx.x * groups + gi; it < items; it += (long long)gridDim.x * groups) {
-        const unsigned per = 2u * (unsigned)s.H * (unsigned)a.touched;
-        const int b = (int)(it / per);
-        const unsigned rest = (unsigned)(it - (long long)b * per), x = rest / (2u * (unsigned)s.H), h2 = rest - x * (2u * (unsigned)s.H);
-        const int h = (int)(h2 >> 1), side = (int)(h2 & 1);
-        const StoreRow r = store_row(a, b, !a.append ? 0 : s.B <= 32 ? held_s[b] : a.c.state[b * kQ8State]);
-        if (!r.goes) continue;
-        const int blk = r.first + (int)x, k0 = r.held & (s.blk - 1);
-        const bool two = k0 > 0 && r.whole > r.first;                // the tail is read and written
-        const bool completes = blk < r.whole, fills = (r.total & (s.blk - 1)) != 0 && (two ? x == 0 : blk == r.whole);
-        if (!completes && !fills) continue;
+    const StoreRow r = store_row(a, b, held);
+    const int x0 = (int)blockIdx.x * a.run * groups + gi;            // the group's blocks: x0, x0 + groups, ...
+    const int k0 = r.held & (s.blk - 1);
+    const bool two = k0 > 0 && r.whole > r.first;                    // the tail is read and written
+    if (r.goes && r.first + (int)blockIdx.x * a.run * groups <= r.whole) {
         const int32_t* table = a.c.table + (size_t)b * s.nb;
         T* tail = reinterpret_cast<T*>(side ? a.c.v_tail : a.c.k_tail) + (((size_t)b * s.H + h) * (size_t)s.blk << a.ld);
         const T* src = (side ? a.V : a.K) + (int64_t)b * a.sb + (int64_t)h * a.sh;
-        if (completes) {
-            const int page = table[blk];
-            const bool good = page >= 0 && page < s.n_pages;
-            if (!good && gt == 0) q8_report(a.c.status, FA_ERR_INDEX);
-            Vec16<T> v[NV];
-            uint32_t m = 0;
+        constexpr bool kAhead = NV * sizeof(T) <= 8;                 // (the next block's values in registers too)
+        Vec16<T> v[NV], y[kAhead ? NV : 1];
+        auto load = [&](Vec16<T>* to, int blk) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 const int i = gt + k * group, t = i >> lv, e = (i & ((1 << lv) - 1)) << 4;
                 const int at = (blk << s.lb) + t;                    // the token's place in the row
-                v[k].load(at < r.held ? tail + ((size_t)t << a.ld) + e : src + (int64_t)(at - r.held) * a.st + e);
+                to[k].load(at < r.held ? tail + ((size_t)t << a.ld) + e : src + (int64_t)(at - r.held) * a.st + e);
             }
-#pragma unroll
-            for (int k = 0; k < NV; ++k) m = max(m, v[k].amax_bits());
-            m = group_max(m);
-            if (good) {
-                const Q8Round<FMT, T> to(m);
-                const size_t ph = (size_t)page * s.H + h;
-                uint8_t* out = (side ? a.c.v_pages : a.c.k_pages) + (ph * (size_t)s.blk << a.ld);
-#pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    uint4 o;
-                    o.x = to.pack(v[k].at(0), v[k].at(1), v[k].at(2), v[k].at(3));
-                    o.y = to.pack(v[k].at(4), v[k].at(5), v[k].at(6), v[k].at(7));
-                    o.z = to.pack(v[k].at(8), v[k].at(9), v[k].at(10), v[k].at(11));
-                    o.w = to.pack(v[k].at(12), v[k].at(13), v[k].at(14), v[k].at(15));
-                    *reinterpret_cast<uint4*>(out + (size_t)(gt + k * group) * 16) = o;
+        };
+        if (kAhead && r.first + x0 < r.whole) load(v, r.first + x0);
+        for (int i = 0; i < a.run; ++i) {
+            const int x = x0 + i * groups, blk = r.first + x;
+            if (blk < r.whole) {                                     // completed by the call
+                const int page = table[blk];
+                if constexpr (kAhead) {
+                    if (i + 1 < a.run && blk + groups < r.whole) load(y, blk + groups);
+                } else {
+                    load(v, blk);
                 }
-                if (gt == 0) (side ? a.c.v_scale : a.c.k_scale)[ph] = Q8Round<FMT, T>::scale(m);
+                uint32_t m = 0;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) m = max(m, v[k].amax_bits());
+                m = group_max(m);
+                if (page >= 0 && page < s.n_pages) {
+                    const Q8Round<FMT, T> to(m);
+                    const size_t ph = (size_t)page * s.H + h;
+                    uint8_t* out = (side ? a.c.v_pages : a.c.k_pages) + (ph * (size_t)s.blk << a.ld);
+#pragma unroll
+                    for (int k = 0; k < NV; ++k) {
+                        uint4 o;
+                        o.x = to.pack(v[k].at(0), v[k].at(1), v[k].at(2), v[k].at(3));
+                        o.y = to.pack(v[k].at(4), v[k].at(5), v[k].at(6), v[k].at(7));
+                        o.z = to.pack(v[k].at(8), v[k].at(9), v[k].at(10), v[k].at(11));
+                        o.w = to.pack(v[k].at(12), v[k].at(13), v[k].at(14), v[k].at(15));
+                        *reinterpret_cast<uint4*>(out + (size_t)(gt + k * group) * 16) = o;
+                    }
+                    if (gt == 0) (side ? a.c.v_scale : a.c.k_scale)[ph] = Q8Round<FMT, T>::scale(m);
+                } else if (gt == 0) {
+                    q8_report(a.c.status, FA_ERR_INDEX);
+                }
+                if constexpr (kAhead)
+#pragma unroll
+                    for (int k = 0; k < NV; ++k) v[k] = y[k];
             }
-        }
-        if (fills) {
-            // the tail stays as it is if any block of the row has no page; the group decides as one
-            if (group_max(pages_there(a, b, r, gt, group) ? 0u : 1u)) continue;
-            // the row's new tokens from t0 on, behind the n0 that the tail has of this block
-            const int t0 = max(r.held, r.whole << s.lb), n0 = r.whole > r.first ? 0 : k0;
-            const int nv = (r.total - t0) << lv;
-            uint32_t m = 0;
-            for (int i = gt; i < nv; i += group) {
-                const int t = i >> lv, e = (i & ((1 << lv) - 1)) << 4;
-                Vec16<T> v;
-                v.load(src + (int64_t)(t0 - r.held + t) * a.st + e);
-                v.store(tail + ((size_t)(n0 + t) << a.ld) + e);
-                m = max(m, v.amax_bits());
-            }
-            m = group_max(m);
-            if (gt == 0) {
-                float* amax = a.c.tail_amax + ((size_t)b * s.H + h) * 2 + side;
-                const float before = n0 > 0 ? *amax : 0.f;
-                *amax = __uint_as_float(max(m, __float_as_uint(before)));
+            if ((r.total & (s.blk - 1)) != 0 && (two ? x == 0 : blk == r.whole)) {
+                // what stays incomplete; the tail stays as it is if any block of the row has no page (the group decides as one)
+                if (group_max(pages_there(a, b, r, gt, group) ? 0u : 1u)) continue;
+                // the row's new tokens from t0 on, behind the n0 that the tail has of this block
+                const int t0 = max(r.held, r.whole << s.lb), n0 = r.whole > r.first ? 0 : k0;
+                const int nv = (r.total - t0) << lv;
+                uint32_t m = 0;
+                for (int j = gt; j < nv; j += group) {
+                    const int t = j >> lv, e = (j & ((1 << lv) - 1)) << 4;
+                    Vec16<T> w;
+                    w.load(src + (int64_t)(t0 - r.held + t) * a.st + e);
+                    w.store(tail + ((size_t)(n0 + t) << a.ld) + e);
+                    m = max(m, w.amax_bits());
+                }
+                m = group_max(m);
+                if (gt == 0) {
+                    float* amax = a.c.tail_amax + ((size_t)b * s.H + h) * 2 + side;
+                    const float before = n0 > 0 ? *amax : 0.f;
+                    *amax = __uint_as_float(max(m, __float_as_uint(before)));
+                }
             }
         }
     }
     // ---- the rows' lengths: nobody reads them in a write ----
-    if (a.append && s.B > 32) {                                      // (the loop above has read them)
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) last_s = atomicInc(reinterpret_cast<unsigned*>(a.c.status) + 1, gridDim.x - 1) == gridDim.x - 1;
-    }
     __syncthreads();
-    if (a.append ? !last_s : blockIdx.x != gridDim.x - 1) return;
+    if (a.append ? !last_s : blockIdx.x + blockIdx.y + blockIdx.z != 0) return;
     const int cap = s.nb << s.lb;
-    for (int b = warp; b < s.B; b += kStoreThreads / 32) {
-        int32_t* st = a.c.state + b * kQ8State;
-        const StoreRow r = store_row(a, b, a.append ? st[0] : 0);
-        const bool there = __all_sync(0xffffffffu, pages_there(a, b, r, lane, 32));
+    for (int i = warp; i < s.B; i += kStoreThreads / 32) {
+        int32_t* st = a.c.state + i * kQ8State;
+        const StoreRow q = store_row(a, i, a.append ? st[0] : 0);
+        const bool there = __all_sync(0xffffffffu, pages_there(a, i, q, lane, 32));
         if (lane != 0) continue;
-        const int n = a.n_row ? a.n_row[b] : a.n;
-        if (r.held < 0 || r.held > cap || min(n, a.n) > cap - r.held) q8_report(a.c.status, FA_ERR_CAPACITY);
-        else if (there) st[0] = r.total;
+        const int n = a.n_row ? a.n_row[i] : a.n;
+        if (q.held < 0 || q.held > cap || min(n, a.n) > cap - q.held) q8_report(a.c.status, FA_ERR_CAPACITY);
+        else if (there) st[0] = q.total;
         else if (!a.append) st[0] = 0;                               // (pages of its blocks may have been written)
     }
 }
@@ -251,20 +251,24 @@ __global__ void __launch_bounds__(256) q8_read_kernel(Q8Dims s, Q8Cache c, T* __
 }
 
 template <typename T, int FMT, int NV>
-cudaError_t store_launch(const StoreArgs<T>& a, cudaStream_t stream) {
+cudaError_t store_launch(StoreArgs<T> a, long long touched, cudaStream_t stream) {
     const int groups = kStoreThreads * NV * 16 / (a.s.blk * a.s.d);
-    const long long items = (long long)a.s.B * a.touched * 2 * a.s.H, need = (items + groups - 1) / groups, most = (long long)sm_count() * 8;
-    return launch_behind(q8_store_kernel<T, FMT, NV>, dim3((unsigned)(need < most ? need : most)), kStoreThreads, 0, stream, a);
+    // runs of up to 8 blocks, as long as there are eight CTAs for each SM
+    const long long ctas = (touched + groups - 1) / groups * 2 * a.s.H * a.s.B, run = ctas / (8 * sm_count());
+    a.run = (int)(run < 1 ? 1 : run > 8 ? 8 : run);
+    const long long per = (long long)a.run * groups;
+    return launch_behind(q8_store_kernel<T, FMT, NV>, dim3((unsigned)((touched + per - 1) / per), (unsigned)(2 * a.s.H), (unsigned)a.s.B), kStoreThreads, 0, stream, a);
 }
 template <typename T, int FMT>
 cudaError_t store_of(const Q8Dims& s, const Q8Cache& c, const void* K, const void* V, int64_t sb, int64_t st, int64_t sh, int n, const int32_t* n_row,
                      bool append, cudaStream_t stream) {
     // blocks that n tokens can touch behind a tail of blk - 1
     const int64_t touched = n == 0 ? 1 : ((int64_t)(append ? s.blk - 1 : 0) + n - 1) / s.blk + 1;
-    const StoreArgs<T> a = {s, c, static_cast<const T*>(K), static_cast<const T*>(V), sb, st, sh, n, n_row, append, (int)touched, s.d == 64 ? 6 : s.d == 128 ? 7 : 8};
+    const StoreArgs<T> a = {s, c, static_cast<const T*>(K), static_cast<const T*>(V), sb, st, sh, n, n_row, append, 1, s.d == 64 ? 6 : s.d == 128 ? 7 : 8};
     // 32 values to a thread, so that a block of the smallest size is a warp's; 64 or 128 where it is more than 256 threads'
     const int values = s.blk * s.d;
-    return values <= 8192 ? store_launch<T, FMT, 2>(a, stream) : values <= 16384 ? store_launch<T, FMT, 4>(a, stream) : store_launch<T, FMT, 8>(a, stream);
+    return values <= 8192 ? store_launch<T, FMT, 2>(a, touched, stream)
+                          : values <= 16384 ? store_launch<T, FMT, 4>(a, touched, stream) : store_launch<T, FMT, 8>(a, touched, stream);
 }
 template <typename T, int FMT, int D>
 cudaError_t read_of(const Q8Dims& s, const Q8Cache& c, void* K, void* V, int64_t sb, int64_t st, int64_t sh, int t0, int n, cudaStream_t stream) {
