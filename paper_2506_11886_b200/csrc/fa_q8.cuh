@@ -245,15 +245,24 @@ __device__ __forceinline__ uint32_t q8_halves(uint32_t w, int hi) {
 }
 template <int FMT>
 __device__ __forceinline__ uint32_t q8_flip(uint32_t w) { return FMT == FA_Q8_INT8 ? w ^ 0x80808080u : w; }
+// Four of them times f, each with one rounding.
 template <int FMT>
-__device__ __forceinline__ void q8_floats(uint32_t w, float (&f)[4]) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t h = q8_halves<FMT>(q8_flip<FMT>(w), i);
-        const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h));
-        f[2 * i] = x.x;
-        f[2 * i + 1] = x.y;
+__device__ __forceinline__ void q8_floats(uint32_t w, float f, float (&x)[4]) {
+    Q8Two<float> lo, hi;
+    if constexpr (FMT == FA_Q8_INT8) {
+        const uint32_t u = q8_flip<FMT>(w);                // q + 128 as the last bits of 2^23 + 128 + q
+        const Q8Two<float> less = Q8Two<float>::of(-8388736.f, -8388736.f);
+        lo = Q8Two<float>::of(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441))).plus(less);
+        hi = Q8Two<float>::of(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443))).plus(less);
+    } else {
+        const uint32_t a = q8_halves<FMT>(w, 0), b = q8_halves<FMT>(w, 1);
+        const float2 fa = __half22float2(*reinterpret_cast<const __half2*>(&a)), fb = __half22float2(*reinterpret_cast<const __half2*>(&b));
+        lo = Q8Two<float>::of(fa.x, fa.y);
+        hi = Q8Two<float>::of(fb.x, fb.y);
     }
+    const Q8Two<float> ff = Q8Two<float>::of(f, f);
+    lo.times(ff).get(x[0], x[1]);
+    hi.times(ff).get(x[2], x[3]);
 }
 #endif  // __CUDACC__
 

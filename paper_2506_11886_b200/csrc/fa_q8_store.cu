@@ -180,17 +180,21 @@ __global__ void __launch_bounds__(kStoreThreads, NV * sizeof(T) == 4 ? 3 : NV * 
     }
 }
 
-// A CTA reads kReadPass x 256 pieces of one head for K and V, a piece being 16 bytes of what is written: whole lines on both sides.
-constexpr int kReadPass = 4;
+// A CTA reads the same tokens of one head for K and V.  A thread's piece is 16 bytes of bf16 tensors' pages, two pieces for each side; neighbouring lanes exchange
+// halves of what they write, so that a store covers whole sectors.  Of fp32 tensors it is what 16 written bytes take, four pieces.
+template <typename T>
+constexpr int kReadE = sizeof(T) == 2 ? 16 : 4;             // values of a piece
+template <typename T>
+constexpr int kReadPass = sizeof(T) == 2 ? 2 : 4;
 template <typename T, int FMT, int D>
 __global__ void __launch_bounds__(256) q8_read_kernel(Q8Dims s, Q8Cache c, T* __restrict__ K, T* __restrict__ V, int64_t sb, int64_t st, int64_t sh, int t0,
                                                       int n) {
-    constexpr int kE = 16 / (int)sizeof(T), kTok = 256 * kE / D;     // values of a piece; tokens that a pass of the CTA covers
-    using Bytes = typename std::conditional<kE == 8, uint2, uint32_t>::type;
+    constexpr int kE = kReadE<T>, kPass = kReadPass<T>, kTok = 256 * kE / D;                 // tokens that a pass of the CTA covers
+    using Bytes = typename std::conditional<kE == 16, uint4, uint32_t>::type;
     asm volatile("griddepcontrol.launch_dependents;");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int h = (int)(blockIdx.x % (unsigned)s.H), b = blockIdx.y;
-    const int t1 = t0 + (int)(blockIdx.x / (unsigned)s.H) * (kReadPass * kTok) + (int)threadIdx.x / (D / kE), e = (threadIdx.x % (D / kE)) * kE;
+    const int t1 = t0 + (int)(blockIdx.x / (unsigned)s.H) * (kPass * kTok) + (int)threadIdx.x / (D / kE), e = (threadIdx.x % (D / kE)) * kE;
     const int len = c.state[b * kQ8State];
     if (len < 0 || len > s.nb << s.lb) {
         if (threadIdx.x == 0) q8_report(c.status, FA_ERR_CAPACITY);
@@ -198,11 +202,11 @@ __global__ void __launch_bounds__(256) q8_read_kernel(Q8Dims s, Q8Cache c, T* __
     }
     const int stop = min(len, t0 + n), paged = len >> s.lb << s.lb;
     T* const out[2] = {K + (int64_t)b * sb + (int64_t)h * sh + e, V + (int64_t)b * sb + (int64_t)h * sh + e};
-    Bytes w[2][kReadPass];
-    float f[2][kReadPass];
-    bool there[kReadPass];
+    Bytes w[2][kPass];
+    float f[2][kPass];
+    bool there[kPass];
 #pragma unroll
-    for (int p = 0; p < kReadPass; ++p) {
+    for (int p = 0; p < kPass; ++p) {
         const int t = t1 + p * kTok;
         there[p] = t < stop && t < paged;
         if (there[p]) {
@@ -220,31 +224,41 @@ __global__ void __launch_bounds__(256) q8_read_kernel(Q8Dims s, Q8Cache c, T* __
         }
     }
 #pragma unroll
-    for (int p = 0; p < kReadPass; ++p) {
+    for (int p = 0; p < kPass; ++p) {
         const int t = t1 + p * kTok;
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
-            uint4* to = reinterpret_cast<uint4*>(out[side] + (int64_t)(t - t0) * st);
-            if (there[p]) {
+            T* to = out[side] + (int64_t)(t - t0) * st;
+            if (there[p]) {                                          // (the lanes of a token agree)
                 float x[4];
-                if constexpr (kE == 8) {
-                    uint32_t o[4];
+                if constexpr (kE == 16) {
+                    const uint32_t ws[4] = {w[side][p].x, w[side][p].y, w[side][p].z, w[side][p].w};
+                    uint32_t o[8];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        q8_floats<FMT>(i ? w[side][p].y : w[side][p].x, x);
-                        const __nv_bfloat162 lo = __floats2bfloat162_rn(x[0] * f[side][p], x[1] * f[side][p]);
-                        const __nv_bfloat162 hi = __floats2bfloat162_rn(x[2] * f[side][p], x[3] * f[side][p]);
+                    for (int i = 0; i < 4; ++i) {
+                        q8_floats<FMT>(ws[i], f[side][p], x);
+                        const __nv_bfloat162 lo = __floats2bfloat162_rn(x[0], x[1]), hi = __floats2bfloat162_rn(x[2], x[3]);
                         o[2 * i] = *reinterpret_cast<const uint32_t*>(&lo);
                         o[2 * i + 1] = *reinterpret_cast<const uint32_t*>(&hi);
                     }
-                    *to = make_uint4(o[0], o[1], o[2], o[3]);
+                    // the even lane gives its second 16 bytes for the odd lane's first: the first store is the even lane's 32 bytes, by both
+                    const bool odd = threadIdx.x & 1;
+                    const unsigned both = 3u << (threadIdx.x & 30);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t got = __shfl_xor_sync(both, odd ? o[i] : o[4 + i], 1);
+                        if (odd) { o[i] = got; } else { o[4 + i] = got; }
+                    }
+                    *reinterpret_cast<uint4*>(to + (odd ? -8 : 0)) = make_uint4(o[0], o[1], o[2], o[3]);
+                    *reinterpret_cast<uint4*>(to + (odd ? 8 : 16)) = make_uint4(o[4], o[5], o[6], o[7]);
                 } else {
-                    q8_floats<FMT>(w[side][p], x);
-                    *reinterpret_cast<float4*>(to) = make_float4(x[0] * f[side][p], x[1] * f[side][p], x[2] * f[side][p], x[3] * f[side][p]);
+                    q8_floats<FMT>(w[side][p], f[side][p], x);
+                    *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
                 }
             } else if (t >= paged && t < stop) {                     // the tail: as it is
                 const T* tail = reinterpret_cast<const T*>(side ? c.v_tail : c.k_tail) + (((size_t)b * s.H + h) * (size_t)s.blk + (t - paged)) * D + e;
-                *to = *reinterpret_cast<const uint4*>(tail);
+#pragma unroll
+                for (int i = 0; i < kE * (int)sizeof(T) / 16; ++i) *(reinterpret_cast<uint4*>(to) + i) = *(reinterpret_cast<const uint4*>(tail) + i);
             }
         }
     }
@@ -272,7 +286,7 @@ cudaError_t store_of(const Q8Dims& s, const Q8Cache& c, const void* K, const voi
 }
 template <typename T, int FMT, int D>
 cudaError_t read_of(const Q8Dims& s, const Q8Cache& c, void* K, void* V, int64_t sb, int64_t st, int64_t sh, int t0, int n, cudaStream_t stream) {
-    const int tok = kReadPass * 256 * (16 / (int)sizeof(T)) / D;
+    const int tok = kReadPass<T> * 256 * kReadE<T> / D;
     const int64_t tiles = ((int64_t)n + tok - 1) / tok;
     return launch_behind(q8_read_kernel<T, FMT, D>, dim3((unsigned)(tiles * s.H), (unsigned)s.B), 256, 0, stream, s, c, static_cast<T*>(K), static_cast<T*>(V), sb, st, sh, t0, n);
 }
