@@ -239,7 +239,8 @@ __device__ __forceinline__ uint32_t q8_halves(uint32_t w, int hi) {
         const uint32_t u = hi ? __byte_perm(w, 0x64646464u, 0x4342) : __byte_perm(w, 0x64646464u, 0x4140);   // halves of 1024 + 128 + q
         asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(u), "r"(0x64806480u));
     } else {
-        asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %1;\n cvt.rn.f16x2.e4m3x2 %0, lo;\n}\n" : "=r"(r) : "r"(hi ? w >> 16 : w));
+        if (hi) asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %1;\n cvt.rn.f16x2.e4m3x2 %0, b;\n}\n" : "=r"(r) : "r"(w));
+        else asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %1;\n cvt.rn.f16x2.e4m3x2 %0, a;\n}\n" : "=r"(r) : "r"(w));
     }
     return r;
 }

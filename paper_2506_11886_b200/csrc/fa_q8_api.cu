@@ -18,6 +18,7 @@ fa_status check_q8_layout(const fa_q8_layout* l) {
     if (l->n_q_heads / l->n_kv_heads > 16) return FA_ERR_UNSUPPORTED;
     if (l->batch > 65535 || l->n_kv_heads > 4096) return FA_ERR_UNSUPPORTED;
     if ((int64_t)l->max_blocks * l->block > (1 << 30)) return FA_ERR_UNSUPPORTED;         // token counts are 32 bits
+    if ((int64_t)l->n_pages * l->n_kv_heads * (l->block / 16) >= 0xfffffffell) return FA_ERR_UNSUPPORTED;      // 16 tokens of a head are counted in 32 bits
     return FA_OK;
 }
 

@@ -121,14 +121,14 @@ template <int D>
 __device__ __forceinline__ int k_dim(int c, int t) { return D == 64 ? 16 * t : 128 * (c >> 1) + 32 * t + 16 * (c & 1); }
 
 template <int D>
-__device__ __forceinline__ void issue_unit(uint32_t stage, const uint8_t* kp, const uint8_t* vp, const float* ks, const float* vs, int lane) {
+__device__ __forceinline__ void issue_unit(uint32_t stage, const uint8_t* kp, const uint8_t* vp, const float* scale, int lane) {   // scale: lane 0 K's, lane 1 V's
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
         const int l = i * 32 + lane, off = unit_offset<D>(l / (D / 16), l % (D / 16));
         cp16(stage + off, kp + 16 * l);
         cp16(stage + 16 * D + off, vp + 16 * l);
     }
-    if (lane < 2) cp4(stage + 32 * D + 4 * lane, lane ? vs : ks);
+    if (lane < 2) cp4(stage + 32 * D + 4 * lane, scale);
 }
 
 // The columns of a segment as a warp holds them.
@@ -141,6 +141,7 @@ struct Columns {
     float f[NT][2];                  // columns 2 t, 2 t + 1: logits (base 2) per product
     int last[NT][2];                 // the last token they see
     float m[NT][2], mp[NT][2], l[NT][2];
+    float g[NT][2];                  // 2^(m - m' + 15)
     float o[NT][kMt][4];
 
     __device__ __forceinline__ void mma_s(float (&s)[NT][4], int kt, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) const {
@@ -150,21 +151,26 @@ struct Columns {
             if constexpr (kF32) mma16816(s[nt], a0, a1, a2, a3, ql[nt][kt][0], ql[nt][kt][1]);
         }
     }
-    // Scores of a unit (as products) to weights; tok: the token of row g; stop: tokens of the row (masks only if `edge`).
+    // The factor between p and the weights of V of scale 1.  m' <= m + 128 and m' >= m - 126: only the upper end can leave the range, for V scales
+    // below 2^-111, where the weights then use less of it.
+    __device__ __forceinline__ void factor(int nt, int k) { g[nt][k] = pow2i((int)fminf(fmaxf(m[nt][k] - mp[nt][k] + 15.f, -126.f), 126.f)); }
+    // Scores of a unit (as products) to weights; tok: the token of row g (masks only if `edge`).
     __device__ __forceinline__ void weights(float (&s)[NT][4], float ks, float vs, int tok, bool edge, uint32_t (&w)[NT][2], uint32_t (&wl)[NT][2]) {
-        const int ev = exponent_of(vs) + 1;
+        const float ev = (float)(exponent_of(vs) + 1);
+        ks = fmaf(vs, 0.f, ks);      // (a V scale that is NaN makes the scores so)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const float f0 = f[nt][0] * ks, f1 = f[nt][1] * ks;
             float (&x)[4] = s[nt];
             x[0] *= f0; x[1] *= f1; x[2] *= f0; x[3] *= f1;
-            bool h0 = false, h1 = false, h2 = false, h3 = false;
-            if (edge) {
-                h0 = tok > last[nt][0]; h1 = tok > last[nt][1]; h2 = tok + 8 > last[nt][0]; h3 = tok + 8 > last[nt][1];
-                x[0] = h0 ? -INFINITY : x[0]; x[1] = h1 ? -INFINITY : x[1]; x[2] = h2 ? -INFINITY : x[2]; x[3] = h3 ? -INFINITY : x[3];
+            if (edge) {              // (p and w are 0: the factors are finite)
+                x[0] = tok > last[nt][0] ? -INFINITY : x[0];
+                x[1] = tok > last[nt][1] ? -INFINITY : x[1];
+                x[2] = tok + 8 > last[nt][0] ? -INFINITY : x[2];
+                x[3] = tok + 8 > last[nt][1] ? -INFINITY : x[3];
             }
             const float b0 = fmaxf(x[0], x[2]), b1 = fmaxf(x[1], x[3]);
-            const bool up = b0 > m[nt][0] || b1 > m[nt][1] || b0 + (float)ev > mp[nt][0] || b1 + (float)ev > mp[nt][1];
+            const bool up = b0 > m[nt][0] || b1 > m[nt][1] || b0 + ev > mp[nt][0] || b1 + ev > mp[nt][1];
             if (__any_sync(0xffffffffu, up)) {
                 float c0 = b0, c1 = b1;
 #pragma unroll
@@ -174,22 +180,22 @@ struct Columns {
                 }
                 c0 = ceilf(c0); c1 = ceilf(c1);
                 const float m0 = fmaxf(m[nt][0], c0), m1 = fmaxf(m[nt][1], c1);
-                const float p0 = fmaxf(mp[nt][0], c0 + (float)ev), p1 = fmaxf(mp[nt][1], c1 + (float)ev);
+                const float p0 = fmaxf(mp[nt][0], c0 + ev), p1 = fmaxf(mp[nt][1], c1 + ev);
                 l[nt][0] *= pow2_down(m[nt][0], m0);
                 l[nt][1] *= pow2_down(m[nt][1], m1);
                 const float r0 = pow2_down(mp[nt][0], p0), r1 = pow2_down(mp[nt][1], p1);
 #pragma unroll
                 for (int i = 0; i < kMt; ++i) { o[nt][i][0] *= r0; o[nt][i][1] *= r1; o[nt][i][2] *= r0; o[nt][i][3] *= r1; }
                 m[nt][0] = m0; m[nt][1] = m1; mp[nt][0] = p0; mp[nt][1] = p1;
+                factor(nt, 0);
+                factor(nt, 1);
             }
             const float p0 = ex2(x[0] - m[nt][0]), p1 = ex2(x[1] - m[nt][1]), p2 = ex2(x[2] - m[nt][0]), p3 = ex2(x[3] - m[nt][1]);
             l[nt][0] += p0 + p2;
             l[nt][1] += p1 + p3;
-            // m' <= m + 128 and m' >= m - 126: only the upper end can leave the range, for a V scale below 2^-111, where the weights then use less of it
-            const float most = (float)min(126, 126 - ev);
-            const float c0 = vs * pow2i((int)fminf(fmaxf(m[nt][0] - mp[nt][0] + 15.f, -126.f), most));
-            const float c1 = vs * pow2i((int)fminf(fmaxf(m[nt][1] - mp[nt][1] + 15.f, -126.f), most));
-            const float w0 = h0 ? 0.f : p0 * c0, w1 = h1 ? 0.f : p1 * c1, w2 = h2 ? 0.f : p2 * c0, w3 = h3 ? 0.f : p3 * c1;
+            // (a block whose scores are far below m may have a scale beyond the range: its p are zero then)
+            const float c0 = fminf(vs * g[nt][0], 0x1p127f), c1 = fminf(vs * g[nt][1], 0x1p127f);
+            const float w0 = p0 * c0, w1 = p1 * c1, w2 = p2 * c0, w3 = p3 * c1;
             const uint32_t u0 = half2_of(w0, w1), u1 = half2_of(w2, w3);
             w[nt][0] = movmatrix_t(u0);
             w[nt][1] = movmatrix_t(u1);
@@ -625,25 +631,24 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
                 else qv[nt][c].zero();
             }
         }
-        auto page_of = [&](int u) {
-            if (u >= stop) return -1;
-            const int p = table[u >> lu];
-            if (p >= 0 && p < s.n_pages) return p;
-            if (lane == 0) q8_report(a.c.status, FA_ERR_INDEX);
+        const float* scales = lane ? a.c.v_scale : a.c.k_scale;
+        auto page_of = [&](int u) { return u < stop ? __ldg(table + (u >> lu)) : -1; };
+        auto checked = [&](int u, int p) {                 // -1 for a page that is not there
+            if ((unsigned)p < (unsigned)s.n_pages) return p;
+            if (u < stop && lane == 0) q8_report(a.c.status, FA_ERR_INDEX);
             return -1;
         };
         auto issue = [&](int stage, int u, int page) {
             if (page >= 0) {
-                const size_t ph = (size_t)page * s.H + h;
-                const size_t at = (ph * (size_t)s.blk + (size_t)(u & ((1 << lu) - 1)) * kUnit) * D;
-                issue_unit<D>(ring + (uint32_t)(stage * R::kBytes), a.c.k_pages + at, a.c.v_pages + at, a.c.k_scale + ph, a.c.v_scale + ph, lane);
+                const uint32_t ph = (uint32_t)page * (uint32_t)s.H + (uint32_t)h, at = (ph << lu) + (uint32_t)(u & ((1 << lu) - 1));         // (counted in units)
+                issue_unit<D>(ring + (uint32_t)(stage * R::kBytes), a.c.k_pages + (size_t)at * (kUnit * D), a.c.v_pages + (size_t)at * (kUnit * D), scales + ph, lane);
             }
             cp_commit();
         };
         constexpr int kAhead = R::kStages - 1;
         int u = s0 + warp, pages[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) pages[i] = page_of(u + i * kWarps);
+        for (int i = 0; i < kAhead; ++i) pages[i] = checked(u + i * kWarps, page_of(u + i * kWarps));
         Tail<T> tl = {kt, vt, nullptr, nullptr, row.len - row.first, -1, 0u, 0u};
         bool tail = s1 > paged && row.first + warp * kUnit < min(row.len, seen);       // this warp has a unit of the tail
         bool whole = false;                                                             // which a step has just completed
@@ -665,7 +670,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
                     whole = true;
                     if (tail) {
                         const size_t at = (ph * (size_t)s.blk + (size_t)warp * kUnit) * D;
-                        issue_unit<D>(ring, a.c.k_pages + at, a.c.v_pages + at, a.c.k_scale + ph, a.c.v_scale + ph, lane);
+                        issue_unit<D>(ring, a.c.k_pages + at, a.c.v_pages + at, scales + ph, lane);
                     }
                 }
             } else {
@@ -706,6 +711,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
                 C.last[nt][k] = __shfl_sync(0xffffffffu, lastq, (2 * t + k) * 4);
                 C.m[nt][k] = C.mp[nt][k] = kNegBig;
                 C.l[nt][k] = 0.f;
+                C.factor(nt, k);
             }
 #pragma unroll
             for (int i = 0; i < kMt; ++i) C.o[nt][i][0] = C.o[nt][i][1] = C.o[nt][i][2] = C.o[nt][i][3] = 0.f;
@@ -727,6 +733,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
             cp_wait<kAhead - 1>();
             __syncwarp();
             const int page2 = page_of(u + (kAhead + 1) * kWarps);
+            page1 = checked(u + kAhead * kWarps, page1);
             issue(stage == 0 ? R::kStages - 1 : stage - 1, u + kAhead * kWarps, page1);          // (the stage read last)
             if (pages[0] >= 0) unit_of_page<T, FMT, D, NT>(C, ring + (uint32_t)(stage * R::kBytes), u * kUnit + g, u * kUnit + kUnit > sure, lane);
 #pragma unroll
