@@ -5,7 +5,8 @@
 // then head dims, and no row is lost to padding of the few columns.  The contraction over head dims may take them in any order as long as
 // q follows it, and the rows of O^T may be any dims: a lane reads its operand rows as 16 consecutive bytes of a token row.
 // 8-bit values are halves exactly; q is scaled by a power of two per column, which makes its bf16 values halves exactly (fp32 q: a high
-// and a low half, two products).
+// and a low half, two products).  With bf16 q, int8 K is taken as q8 + 128 in a half's last bits, that is (q8 + 128) 2^-24, exactly: a subtraction less for two
+// values; 128 times the sum of the column's q goes off the scores in the multiplication by the scale.
 //
 // Scales: a score is multiplied by its block's K scale.  The weight of a token in O is w = p sv 2^(m - m' + 15), sv its block's
 // V scale, m the column's running maximum of the scores, m' that of score + exponent of sv, both rounded up to whole numbers (of log2), so
@@ -134,11 +135,12 @@ __device__ __forceinline__ void issue_unit(uint32_t stage, const uint8_t* kp, co
 // The columns of a segment as a warp holds them.
 template <typename T, int D, int NT>
 struct Columns {
-    static constexpr bool kF32 = sizeof(T) == 4;
     static constexpr int kMt = D / 16;
     uint32_t q[NT][kMt][2];          // column g: dims in the order of the lanes' K bytes
-    uint32_t ql[kF32 ? NT : 1][kF32 ? kMt : 1][2];
+    uint32_t ql[sizeof(T) == 4 ? NT : 1][sizeof(T) == 4 ? kMt : 1][2];
+    static constexpr bool kF32 = sizeof(T) == 4;
     float f[NT][2];                  // columns 2 t, 2 t + 1: logits (base 2) per product
+    float shift[kF32 ? 1 : NT][2];   // 128 times the sum of their q (as halves)
     int last[NT][2];                 // the last token they see
     float m[NT][2], mp[NT][2], l[NT][2];
     float g[NT][2];                  // 2^(m - m' + 15)
@@ -155,6 +157,8 @@ struct Columns {
     // below 2^-111, where the weights then use less of it.
     __device__ __forceinline__ void factor(int nt, int k) { g[nt][k] = pow2i((int)fminf(fmaxf(m[nt][k] - mp[nt][k] + 15.f, -126.f), 126.f)); }
     // Scores of a unit (as products) to weights; tok: the token of row g (masks only if `edge`).
+    // low: products of q8 + 128 in the last bits.
+    template <bool LOW>
     __device__ __forceinline__ void weights(float (&s)[NT][4], float ks, float vs, int tok, bool edge, uint32_t (&w)[NT][2], uint32_t (&wl)[NT][2]) {
         const float ev = (float)(exponent_of(vs) + 1);
         ks = fmaf(vs, 0.f, ks);      // (a V scale that is NaN makes the scores so)
@@ -162,7 +166,12 @@ struct Columns {
         for (int nt = 0; nt < NT; ++nt) {
             const float f0 = f[nt][0] * ks, f1 = f[nt][1] * ks;
             float (&x)[4] = s[nt];
-            x[0] *= f0; x[1] *= f1; x[2] *= f0; x[3] *= f1;
+            if constexpr (LOW) {
+                const float g0 = f0 * 0x1p24f, g1 = f1 * 0x1p24f, o0 = -f0 * shift[nt][0], o1 = -f1 * shift[nt][1];
+                x[0] = fmaf(x[0], g0, o0); x[1] = fmaf(x[1], g1, o1); x[2] = fmaf(x[2], g0, o0); x[3] = fmaf(x[3], g1, o1);
+            } else {
+                x[0] *= f0; x[1] *= f1; x[2] *= f0; x[3] *= f1;
+            }
             if (edge) {              // (p and w are 0: the factors are finite)
                 x[0] = tok > last[nt][0] ? -INFINITY : x[0];
                 x[1] = tok > last[nt][1] ? -INFINITY : x[1];
@@ -217,6 +226,8 @@ struct Columns {
 template <typename T, int FMT, int D, int NT>
 __device__ __forceinline__ void unit_of_page(Columns<T, D, NT>& C, uint32_t stage, int tok, bool edge, int lane) {
     const int g = lane >> 2, t = lane & 3;
+    constexpr bool kLow = FMT == FA_Q8_INT8 && sizeof(T) == 2;
+    auto half_k = [](uint32_t w, int hi) { return kLow ? __byte_perm(w, 0u, hi ? 0x4342 : 0x4140) : q8_halves<FMT>(w, hi); };
     float s[NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
@@ -227,11 +238,11 @@ __device__ __forceinline__ void unit_of_page(Columns<T, D, NT>& C, uint32_t stag
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t x = q8_flip<FMT>(xw[j]), y = q8_flip<FMT>(yw[j]);
-            C.mma_s(s, 4 * c + j, q8_halves<FMT>(x, 0), q8_halves<FMT>(y, 0), q8_halves<FMT>(x, 1), q8_halves<FMT>(y, 1));
+            C.mma_s(s, 4 * c + j, half_k(x, 0), half_k(y, 0), half_k(x, 1), half_k(y, 1));
         }
     }
     uint32_t w[NT][2], wl[NT][2];
-    C.weights(s, lds4(stage + 32 * D), lds4(stage + 32 * D + 4), tok, edge, w, wl);
+    C.template weights<kLow>(s, lds4(stage + 32 * D), lds4(stage + 32 * D + 4), tok, edge, w, wl);
     const uint32_t vst = stage + 16 * D;
 #pragma unroll
     for (int c = 0; c < (D == 64 ? 1 : D / 128); ++c) {
@@ -329,7 +340,7 @@ __device__ __forceinline__ void unit_of_tail(Columns<T, D, NT>& C, const Tail<T>
         }
     }
     uint32_t w[NT][2], wl[NT][2];
-    C.weights(s, ks, vs, first + row0 + g, true, w, wl);
+    C.template weights<false>(s, ks, vs, first + row0 + g, true, w, wl);
 #pragma unroll
     for (int c = 0; c < (D == 64 ? 1 : D / 128); ++c) {
         Vec16<T> v[4];
@@ -704,10 +715,21 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
                         if constexpr (kF32) C.ql[nt][4 * c + j][k] = pair_of(qv[nt][c], 4 * j + 2 * k, f, true);
                     }
             const float fcol = pow2i(e - 13) * (s.scale * kLog2e);
+            float sum = 0.f;
+            if constexpr (!kF32) {
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum += qv[nt][c].at(j) * f;
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                sum *= 128.f;
+            }
             const int lastq = qi < a.n_q ? row.len - a.n_q + qi : -1;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 C.f[nt][k] = __shfl_sync(0xffffffffu, fcol, (2 * t + k) * 4);
+                if constexpr (!kF32) C.shift[nt][k] = __shfl_sync(0xffffffffu, sum, (2 * t + k) * 4);
                 C.last[nt][k] = __shfl_sync(0xffffffffu, lastq, (2 * t + k) * 4);
                 C.m[nt][k] = C.mp[nt][k] = kNegBig;
                 C.l[nt][k] = 0.f;
