@@ -361,7 +361,7 @@ typedef struct fa_q8_cache {
     void*    v_tail;
     float*   tail_amax;           /* [B][H_kv][2] largest magnitude of the tail's K and V (written by the calls) */
     const int32_t* block_table;   /* [B][max_blocks] page of every block                      */
-    int32_t* state;               /* [B][4]: tokens of the row, scratch (zero between calls), 2 spare */
+    int32_t* state;               /* [B][4]: tokens of the row, 3 spare                       */
     int32_t* status;              /* [4]: sticky fa_status word, ticket (zero between calls), 2 spare */
 } fa_q8_cache;
 
@@ -400,7 +400,7 @@ fa_status fa_q8_read(const fa_q8_layout* layout, const fa_q8_cache* cache, void*
 /* Softmax attention of n_q queries a row over the cached tokens.  q: element (b, i, g, e) at b*stride_b + i*stride_i +
  * g*stride_g + e (strides in elements, multiples of 8); out: [B][n_q][H_q][d].  The queries are those of the row's
  * last n_q tokens, whose K and V the cache holds already: query i sees tokens 0 .. len - n_q + i.  A query that sees none (an empty
- * row, or a row of fewer than n_q tokens) gives zeros.  Does not modify the cache.  Tokens whose page is out of range are
+ * row, or a row of fewer than n_q tokens) gives zeros.  out must not overlap q.  Does not modify the cache.  Tokens whose page is out of range are
  * left out and FA_ERR_INDEX is reported. */
 fa_status fa_q8_attention(const fa_q8_layout* layout, const fa_q8_cache* cache, const void* q, int64_t stride_b, int64_t stride_i,
                           int64_t stride_g, void* out, int32_t n_q, void* ws, size_t ws_bytes, void* stream);

@@ -8,7 +8,7 @@
 
 namespace fa {
 
-constexpr int kQ8State = 4;          // int32 words of state per row: tokens, scratch, 2 spare
+constexpr int kQ8State = 4;          // int32 words of state per row: tokens, 3 spare
 constexpr int kQ8MaxCtas = 500;      // CTAs of an attention launch; tickets in the first 4 KiB of the workspace: of groups of parts from 0, of
 constexpr int kQ8GroupTickets = 512; // pairs of many groups from here on, and
 constexpr int kQ8StepTicket = 1023;  // of the CTAs of a step which have read the lengths
@@ -39,6 +39,7 @@ inline Q8Cache make_q8_cache(const fa_q8_cache& c) {
 }
 
 // Launchers.  fmt: fa_q8_format, dtype: fa_dtype.
+cudaError_t launch_q8_reset(const Q8Dims&, const Q8Cache&, cudaStream_t);
 cudaError_t launch_q8_store(const Q8Dims&, const Q8Cache&, int fmt, int dtype, const void* K, const void* V, int64_t sb, int64_t st, int64_t sh, int n,
                             const int32_t* n_row, bool append, cudaStream_t);
 cudaError_t launch_q8_read(const Q8Dims&, const Q8Cache&, int fmt, int dtype, void* K, void* V, int64_t sb, int64_t st, int64_t sh, int t0, int n,

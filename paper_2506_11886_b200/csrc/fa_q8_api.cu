@@ -99,10 +99,7 @@ fa_status fa_q8_reset(const fa_q8_layout* layout, fa_q8_cache* cache, void* stre
     fa_status e = check_q8_layout(layout);
     if (e == FA_OK) e = check_q8_cache(layout, cache);
     if (e != FA_OK) return e;
-    cudaStream_t cs = static_cast<cudaStream_t>(stream);
-    if (cudaMemsetAsync(cache->state, 0, (size_t)layout->batch * kQ8State * 4, cs) != cudaSuccess) return FA_ERR_CUDA;
-    if (cudaMemsetAsync(cache->status, 0, 16, cs) != cudaSuccess) return FA_ERR_CUDA;
-    return FA_OK;
+    return launch_q8_reset(make_q8_dims(*layout), make_q8_cache(*cache), static_cast<cudaStream_t>(stream)) == cudaSuccess ? FA_OK : FA_ERR_CUDA;
 }
 
 fa_status fa_q8_write(const fa_q8_layout* layout, fa_q8_cache* cache, const void* K, const void* V, int64_t stride_b, int64_t stride_t, int64_t stride_h,

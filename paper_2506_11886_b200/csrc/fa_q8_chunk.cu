@@ -29,9 +29,6 @@ using namespace umma;
 constexpr int kRows = 256, kTok = 128;
 constexpr int kConv = 16, kMma = 20, kConvWarps = 7;       // first converting warp, the issuing warp, converting warps (16-19, 21-23)
 constexpr int kChunkThreads = 24 * 32;
-// Registers of a thread of the weights and of the others; together those that the launch has (6 groups of four warps x 80).
-constexpr int kRegsRow = 80, kRegsRest = 80;
-static_assert(4 * kRegsRow + 2 * kRegsRest == 6 * 80, "");
 constexpr int kScSlots = 4;                                // scales of blocks: a slot is free when the weights of the block two in front are done
 
 struct ChunkArgs {
@@ -242,7 +239,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
 
     if (warp < 16) {
         // ---- a tile's weights ----
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsRow));
         const int tile = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         // this thread's scores, whose place its weights take (two to a column), and its half of the columns of O
@@ -462,7 +458,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
         }
     } else if (warp != kMma) {
         // ---- 8-bit values to halves ----
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
         constexpr int kChunks = D / 16, kRowsOf = 32 / kChunks, kItems = kTok / kRowsOf;      // 16-value chunks of a row; rows of a warp's load; loads of a side
         constexpr int kMine = (kItems + kConvWarps - 1) / kConvWarps;                         // ... of a warp
         const int w0 = warp < kMma ? warp - kConv : warp - kConv - 1, ch = lane % kChunks, r0 = lane / kChunks;
@@ -617,7 +612,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
         }
     } else {
         // ---- the MMAs ----
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
         // operands: K-major with 64 dims to a row of 128 bytes, the next 64 a box further; V the same read along the tokens (MN-major)
         const uint64_t qd0 = umma_desc(smem_u32(qs), 1, 1024 >> 4), kd0 = umma_desc(smem_u32(ks), 1, 1024 >> 4);
         const uint64_t vd0 = umma_desc(smem_u32(vs), (kTok * 128) >> 4, 1024 >> 4);

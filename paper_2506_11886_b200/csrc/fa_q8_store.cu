@@ -264,6 +264,14 @@ __global__ void __launch_bounds__(256) q8_read_kernel(Q8Dims s, Q8Cache c, T* __
     }
 }
 
+__global__ void __launch_bounds__(256) q8_reset_kernel(int32_t* __restrict__ state, int n, int32_t* __restrict__ status) {
+    asm volatile("griddepcontrol.launch_dependents;");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < n) state[i] = 0;
+    if (i < 4) status[i] = 0;
+}
+
 template <typename T, int FMT, int NV>
 cudaError_t store_launch(StoreArgs<T> a, long long touched, cudaStream_t stream) {
     const int groups = kStoreThreads * NV * 16 / (a.s.blk * a.s.d);
@@ -308,6 +316,10 @@ cudaError_t read_of(const Q8Dims& s, const Q8Cache& c, void* K, void* V, int64_t
 
 }  // namespace
 
+cudaError_t launch_q8_reset(const Q8Dims& s, const Q8Cache& c, cudaStream_t stream) {
+    const int n = s.B * kQ8State;
+    return launch_behind(q8_reset_kernel, dim3((unsigned)((n + 255) / 256)), 256, 0, stream, c.state, n, c.status);
+}
 cudaError_t launch_q8_store(const Q8Dims& s, const Q8Cache& c, int fmt, int dtype, const void* K, const void* V, int64_t sb, int64_t st, int64_t sh, int n,
                             const int32_t* n_row, bool append, cudaStream_t stream) {
     if (dtype == FA_BF16)

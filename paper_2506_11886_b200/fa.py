@@ -530,6 +530,7 @@ class Q8Cache:
             assert t.numel() * t.element_size() == sizes[n], (n, t.shape, sizes[n])
             setattr(self, n, t)
         self.device = dev
+        self._index = dev.index if dev.index is not None else (torch.cuda.current_device() if dev.type == "cuda" else -1)
         self._c = fa_q8_cache(*[_ptr(getattr(self, n)) for n in _Q8_FIELDS])
         self._cref = C.byref(self._c)
 
@@ -545,16 +546,23 @@ def new_q8_workspace(layout: Q8Layout, n_q: int = 1, device="cuda") -> torch.Ten
     return torch.zeros(fa_q8_workspace_bytes(layout, n_q), dtype=torch.uint8, device=device)
 
 
+def _q8_stream(cache: Q8Cache, stream, what: str) -> int:
+    """The raw stream; a call runs on the current device, which has to be the cache's."""
+    if cache._index < 0 or torch.cuda.current_device() != cache._index:
+        raise ValueError(f"{what}: the cache is on {cache.device}, which is not the current CUDA device")
+    return _stream(stream)
+
+
 def fa_q8_reset(layout: Q8Layout, cache: Q8Cache, stream=None) -> None:
-    _check(lib().fa_q8_reset(layout.ref(), cache._cref, _stream(stream)), "fa_q8_reset")
+    _check(lib().fa_q8_reset(layout.ref(), cache._cref, _q8_stream(cache, stream, "fa_q8_reset")), "fa_q8_reset")
 
 
-def _q8_tokens(layout: Q8Layout, K: torch.Tensor, V: torch.Tensor, what: str):
+def _q8_tokens(layout: Q8Layout, cache: Q8Cache, K: torch.Tensor, V: torch.Tensor, what: str):
     """Strides and count of [B][n][H_kv][d] tensors."""
-    shape = K.shape
+    shape, dev = K.shape, cache._index
     if (len(shape) != 4 or shape[0] != layout.batch or shape[2] != layout.n_kv_heads or shape[3] != layout.head_dim or V.shape != shape
-            or K.dtype != layout.torch_dtype or V.dtype != K.dtype or not K.is_cuda or not V.is_cuda):
-        raise ValueError(f"{what}: K and V have to be [B][n][H_kv][d] tensors of the layout on the GPU")
+            or K.dtype != layout.torch_dtype or V.dtype != K.dtype or dev < 0 or K.get_device() != dev or V.get_device() != dev):
+        raise ValueError(f"{what}: K and V have to be [B][n][H_kv][d] tensors of the layout on the cache's GPU")
     st = K.stride()
     if st != V.stride() or (shape[1] and st[3] != 1):
         raise ValueError(f"{what}: K and V have to have the same strides, 1 along d")
@@ -564,10 +572,11 @@ def _q8_tokens(layout: Q8Layout, K: torch.Tensor, V: torch.Tensor, what: str):
 
 
 def _q8_store(call, what, layout, cache, K, V, n_row, stream):
-    sb, st, sh, n = _q8_tokens(layout, K, V, what)
-    if n_row is not None and (n_row.dtype != torch.int32 or n_row.shape != (layout.batch,) or not n_row.is_cuda or not n_row.is_contiguous()):
-        raise ValueError(f"{what}: n_row has to be an int32 tensor [B] on the GPU")
-    status = call(layout.ref(), cache._cref, K.data_ptr(), V.data_ptr(), sb, st, sh, n, 0 if n_row is None else n_row.data_ptr(), _stream(stream))
+    sb, st, sh, n = _q8_tokens(layout, cache, K, V, what)
+    if n_row is not None and (n_row.dtype != torch.int32 or n_row.shape != (layout.batch,) or n_row.get_device() != cache._index or not n_row.is_contiguous()):
+        raise ValueError(f"{what}: n_row has to be an int32 tensor [B] on the cache's GPU")
+    status = call(layout.ref(), cache._cref, K.data_ptr(), V.data_ptr(), sb, st, sh, n, 0 if n_row is None else n_row.data_ptr(),
+                  _q8_stream(cache, stream, what))
     if status:
         _check(status, what)
 
@@ -584,24 +593,25 @@ def fa_q8_append(layout: Q8Layout, cache: Q8Cache, K: torch.Tensor, V: torch.Ten
 
 def fa_q8_read(layout: Q8Layout, cache: Q8Cache, K: torch.Tensor, V: torch.Tensor, t0: int = 0, stream=None) -> None:
     """Tokens t0 .. t0 + n - 1 into K, V [B][n][H_kv][d]; what a row does not hold stays as it is there."""
-    sb, st, sh, n = _q8_tokens(layout, K, V, "fa_q8_read")
-    status = lib().fa_q8_read(layout.ref(), cache._cref, K.data_ptr(), V.data_ptr(), sb, st, sh, t0, n, _stream(stream))
+    sb, st, sh, n = _q8_tokens(layout, cache, K, V, "fa_q8_read")
+    status = lib().fa_q8_read(layout.ref(), cache._cref, K.data_ptr(), V.data_ptr(), sb, st, sh, t0, n, _q8_stream(cache, stream, "fa_q8_read"))
     if status:
         _check(status, "fa_q8_read")
 
 
 def fa_q8_attention(layout: Q8Layout, cache: Q8Cache, q: torch.Tensor, out: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
     """q [B][n_q][H_q][d] (any strides with unit stride on d), out contiguous [B][n_q][H_q][d]; or [B][H_q][d] both, for one query a row."""
-    shape, st = q.shape, q.stride()
+    shape, st, dev = q.shape, q.stride(), cache._index
     if len(shape) == 3:
         n_q, si = 1, layout.head_dim
     else:
         n_q, si = shape[1], (st[1] if shape[1] > 1 else layout.head_dim)
     if (shape[0] != layout.batch or shape[-2] != layout.n_q_heads or shape[-1] != layout.head_dim or len(shape) not in (3, 4) or out.shape != shape
-            or q.dtype != layout.torch_dtype or out.dtype != q.dtype or not q.is_cuda or not out.is_cuda or not out.is_contiguous() or st[-1] != 1):
-        raise ValueError("fa_q8_attention: q and out have to be [B][n_q][H_q][d] or [B][H_q][d] tensors of the layout on the GPU, out contiguous")
+            or q.dtype != layout.torch_dtype or out.dtype != q.dtype or dev < 0 or q.get_device() != dev or out.get_device() != dev or ws.get_device() != dev
+            or not out.is_contiguous() or st[-1] != 1):
+        raise ValueError("fa_q8_attention: q and out have to be [B][n_q][H_q][d] or [B][H_q][d] tensors of the layout, out contiguous, all on the cache's GPU")
     status = lib().fa_q8_attention(layout.ref(), cache._cref, q.data_ptr(), st[0] if shape[0] > 1 else 0, si, st[-2] if shape[-2] > 1 else layout.head_dim,
-                                   out.data_ptr(), n_q, ws.data_ptr(), ws.numel(), _stream(stream))
+                                   out.data_ptr(), n_q, ws.data_ptr(), ws.numel() * ws.element_size(), _q8_stream(cache, stream, "fa_q8_attention"))
     if status:
         _check(status, "fa_q8_attention")
 
@@ -609,15 +619,18 @@ def fa_q8_attention(layout: Q8Layout, cache: Q8Cache, q: torch.Tensor, out: torc
 def fa_q8_step(layout: Q8Layout, cache: Q8Cache, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, out: torch.Tensor, ws: torch.Tensor,
                stream=None) -> None:
     """fa_q8_append of one token a row (k_new, v_new [B][H_kv][d]) then fa_q8_attention (q, out [B][H_q][d]) as one step."""
+    dev = cache._index
     qs, ks, dt = (layout.batch, layout.n_q_heads, layout.head_dim), (layout.batch, layout.n_kv_heads, layout.head_dim), layout.torch_dtype
     for t, shape in ((q, qs), (k_new, ks), (v_new, ks), (out, qs)):
-        if t.shape != shape or t.dtype != dt or not t.is_cuda or not t.is_contiguous():
-            raise ValueError("fa_q8_step: q, out [B][H_q][d] and k_new, v_new [B][H_kv][d] have to be contiguous tensors of the layout on the GPU")
-    status = lib().fa_q8_step(layout.ref(), cache._cref, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.numel(),
-                              _stream(stream))
+        if t.shape != shape or t.dtype != dt or dev < 0 or t.get_device() != dev or not t.is_contiguous():
+            raise ValueError("fa_q8_step: q, out [B][H_q][d] and k_new, v_new [B][H_kv][d] have to be contiguous tensors of the layout on the cache's GPU")
+    if ws.get_device() != dev:
+        raise ValueError("fa_q8_step: the workspace has to be on the cache's GPU")
+    status = lib().fa_q8_step(layout.ref(), cache._cref, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), out.data_ptr(), ws.data_ptr(),
+                              ws.numel() * ws.element_size(), _q8_stream(cache, stream, "fa_q8_step"))
     if status:
         _check(status, "fa_q8_step")
 
 
 def fa_q8_poll_status(cache: Q8Cache, stream=None) -> int:
-    return int(lib().fa_q8_poll_status(cache._cref, _stream(stream)))
+    return int(lib().fa_q8_poll_status(cache._cref, _q8_stream(cache, stream, "fa_q8_poll_status")))

@@ -428,6 +428,57 @@ def test_rows_may_share_pages_and_pages_may_lie_past_32_bits():
     assert torch.equal(k[0, :256], k[1, :256]) and (k[1, 256:384] != 0).any()
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("n_q", [1, 40])
+def test_pages_of_an_engine(fmt, n_q):
+    """Pages, scales and lengths that did not come from fa_q8_write: any byte (int8 -128 among them; no e4m3 NaN), scales of zero; more than 32 rows."""
+    B, Hq, H, d, block, nb = 40, 4, 2, 128, 32, 6
+    lay, cache = make(B=B, Hq=Hq, H=H, d=d, block=block, nb=nb, fmt=fmt)
+    g = torch.Generator().manual_seed(9)
+    for side in ("k", "v"):
+        raw = torch.randint(0, 256, getattr(cache, side + "_pages").shape, generator=g, dtype=torch.uint8)
+        if fmt == "e4m3":
+            raw[(raw & 0x7f) == 0x7f] = 0x70
+        getattr(cache, side + "_pages").view(torch.uint8).copy_(raw)
+        scale = 0.02 * torch.rand(getattr(cache, side + "_scale").shape, generator=g)
+        scale[::7] = 0
+        getattr(cache, side + "_scale").copy_(scale)
+    lens = [(b * 37) % (nb * block) // block * block for b in range(B)]
+    cache.state[:, 0] = torch.tensor(lens, dtype=torch.int32)
+    q = rand((B, n_q, Hq, d), "bf16", 3)
+    out, ws = torch.full_like(q, float("nan")), fa.new_q8_workspace(lay, n_q)
+    fa.fa_q8_attention(lay, cache, q, out, ws)
+    assert fa.fa_q8_poll_status(cache) == fa.FA_OK
+    table, got = cache.block_table.cpu().long(), out.cpu().double()
+    for b in range(B):
+        for h in range(H):
+            kv = [getattr(cache, s + "_pages")[:, h].cpu()[table[b, :lens[b] // block]].double() * getattr(cache, s + "_scale")[:, h].cpu()[table[b, :lens[b] // block]].double()[:, None, None]
+                  for s in ("k", "v")]
+            k, v = (x.reshape(lens[b], d) for x in kv)
+            want, tol = ref.attention(k, v, q[b, :, 2 * h:2 * h + 2].cpu().double(), n_q, lay.softmax_scale, torch.bfloat16)
+            assert ((got[b, :, 2 * h:2 * h + 2] - want).abs() <= tol).all(), (b, h)
+
+
+def test_a_length_that_is_none_is_refused_row_by_row():
+    lay, cache = make(B=3, H=2, d=64, block=16, nb=2)
+    K = rand((3, 32, 2, 64), "bf16", 1)
+    fa.fa_q8_write(lay, cache, K, K)
+    cache.state[0, 0], cache.state[2, 0] = 33, -1
+    q = rand((3, 1, 8, 64), "bf16", 2)
+    out, ws = torch.full_like(q, float("nan")), fa.new_q8_workspace(lay)
+    fa.fa_q8_attention(lay, cache, q, out, ws)
+    assert fa.fa_q8_poll_status(cache) == fa.FA_ERR_CAPACITY
+    assert (out[0] == 0).all() and (out[2] == 0).all() and torch.isfinite(out[1].float()).all() and (out[1] != 0).any()
+    k = torch.full_like(K, -3.0)
+    fa.fa_q8_read(lay, cache, k, k.clone())
+    assert fa.fa_q8_poll_status(cache) == fa.FA_ERR_CAPACITY and (k[0] == -3).all() and (k[2] == -3).all() and (k[1] != -3).any()
+    fa.fa_q8_step(lay, cache, q[:, 0].contiguous(), K[:, 0].contiguous(), K[:, 1].contiguous(), out[:, 0].contiguous(), ws)
+    assert fa.fa_q8_poll_status(cache) == fa.FA_ERR_CAPACITY
+    assert cache.state[:, 0].tolist() == [33, 32, -1]                       # (row 1 is full)
+    fa.fa_q8_reset(lay, cache)
+    assert (cache.state == 0).all() and fa.fa_q8_poll_status(cache) == fa.FA_OK
+
+
 # ---- steps ------------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 @pytest.mark.parametrize("dtype,d,block", [("bf16", 128, 64), ("f32", 64, 16), ("bf16", 256, 128), ("bf16", 64, 32)])
@@ -435,6 +486,7 @@ def test_a_step_is_an_append_and_an_attention(fmt, dtype, d, block):
     """Bit for bit in the cache; results within the tolerance of the definition; rows of their own lengths, over ends of blocks, from empty ones on."""
     Hq, H = 4, 2
     lens = [0, block - 2, 2 * block - 1, 130]
+    lens = lens + [7 * b % 40 for b in range(32 if dtype == "f32" else 0)]   # (more than 32 rows)
     B, steps = len(lens), 5
     lay, cache = make(B=B, Hq=Hq, H=H, d=d, block=block, nb=260 // block + 2, fmt=fmt, dtype=dtype)
     _, other = make(B=B, Hq=Hq, H=H, d=d, block=block, nb=260 // block + 2, fmt=fmt, dtype=dtype)
