@@ -128,9 +128,10 @@ struct Q8Round {
     using Two = Q8Two<R>;
     static constexpr float kTop = FMT == FA_Q8_INT8 ? 127.f : 448.f;
     R top, minus, inv;               // p top, -p amax, 1 / (p amax)
-    bool live;                       // some value is not zero, all are finite
+    uint32_t keep;                   // all bits if some value is not zero and all are finite; else the bytes are zero
     __device__ __forceinline__ explicit Q8Round(uint32_t amax_bits) {
-        live = amax_bits != 0 && amax_bits < 0x7f800000u;
+        const bool live = amax_bits != 0 && amax_bits < 0x7f800000u;
+        keep = live ? 0xffffffffu : 0u;
         const float p = amax_bits < 0x21800000u ? 0x1p64f : amax_bits > 0x5d800000u ? 0x1p-64f : 1.f;
         const float as = __uint_as_float(amax_bits) * p;
         top = (R)(kTop * p);
@@ -144,7 +145,6 @@ struct Q8Round {
     }
     // Four values to four bytes.
     __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d) const {
-        if (!live) return 0u;
         Two q0 = quotient(a, b), q1 = quotient(c, d);
         R r0, r1, r2, r3;
         uint32_t r;
@@ -163,7 +163,7 @@ struct Q8Round {
                 : "=r"(r)
                 : "f"(narrow(r0)), "f"(narrow(r1)), "f"(narrow(r2)), "f"(narrow(r3)));
         }
-        return r;
+        return r & keep;
     }
     static __device__ __forceinline__ uint32_t last_word(float x) { return __float_as_uint(x); }
     static __device__ __forceinline__ uint32_t last_word(double x) { return (uint32_t)__double2loint(x); }
@@ -201,11 +201,8 @@ struct Vec16<__nv_bfloat16> {
     __device__ __forceinline__ uint32_t amax_bits() const {
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t w = word(i) & 0x7fff7fffu;
-            m = max(m, max(w << 16, w & 0xffff0000u));
-        }
-        return m;
+        for (int i = 0; i < 8; ++i) m = __vmaxu2(m, word(i) & 0x7fff7fffu);
+        return max(m << 16, m & 0xffff0000u);
     }
 };
 template <>
