@@ -15,7 +15,8 @@
 // tiles stand in a line that is cut into equal parts, one for each SM; the parts of a tile that is cut meet in the workspace, and a second kernel
 // joins them, spread over all SMs.
 // The loops of the roles share the instruction cache: what is unrolled (a row of scores in registers) is written once, the rest kept small.
-// Bound by the exponentials (16 a clock and SM: 2048 clocks for a block and 256 rows of any head dim) and, at 128 dims, by as many clocks of the tensor cores.
+// The exponentials (16 a clock and SM) take 2048 clocks for a block and 256 rows of any head dim, the tensor cores as many at 128 dims; it is bound by the chain of a tile
+// (scores, maximum, exponentials, products), 5300 clocks, of which two run at a time: 2048 queries of 32/8 heads of 128 over 16384 tokens 650 us (793 TFLOP/s).
 #include <type_traits>
 
 #include "fa_q8.cuh"
