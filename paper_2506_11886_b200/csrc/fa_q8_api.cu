@@ -38,8 +38,9 @@ fa_status check_tokens(const fa_q8_layout* l, const void* K, const void* V, int6
     if (n == 0) return FA_OK;
     if (!K || !V || !aligned16(K) || !aligned16(V)) return FA_ERR_INVALID_ARG;
     if (sb < 0 || st < l->head_dim || sh < l->head_dim || ((sb | st | sh) & 7)) return FA_ERR_INVALID_ARG;
-    // blocks (of 16 tokens at least) and heads of a launch are counted in 32 bits
-    if (((int64_t)n / 16 + 2) * 2 * l->n_kv_heads > 0x7fffffff) return FA_ERR_UNSUPPORTED;
+    // a launch's blocks of all rows and heads are counted in 32 bits
+    const int64_t blocks = (int64_t)n / l->block + 2, most = (int64_t)l->max_blocks + 1;
+    if ((blocks < most ? blocks : most) * 2 * l->n_kv_heads * l->batch > 0x7fffffff) return FA_ERR_UNSUPPORTED;
     return FA_OK;
 }
 
@@ -119,6 +120,9 @@ fa_status fa_q8_read(const fa_q8_layout* layout, const fa_q8_cache* cache, void*
     if (e == FA_OK) e = check_tokens(layout, K, V, stride_b, stride_t, stride_h, n);
     if (e != FA_OK) return e;
     if (t0 < 0 || n > 0x7fffffff - t0) return FA_ERR_INVALID_ARG;
+    const int32_t cap = layout->max_blocks * layout->block;
+    if (t0 >= cap) return FA_OK;
+    if (n > cap - t0) n = cap - t0;                        // (no row has more)
     if (n == 0) return FA_OK;
     return launch_q8_read(make_q8_dims(*layout), make_q8_cache(*cache), layout->format, layout->kv_dtype, K, V, stride_b, stride_t, stride_h, t0, n,
                           static_cast<cudaStream_t>(stream)) == cudaSuccess ? FA_OK : FA_ERR_CUDA;

@@ -210,7 +210,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
     const Q8Dims& s = a.s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-    asm volatile("griddepcontrol.launch_dependents;");
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar.k_full + i, kConvWarps); mbar_init(bar.k_empty + i, 1); mbar_init(bar.v_full + i, kConvWarps); mbar_init(bar.v_empty + i, 1);
@@ -219,6 +218,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
         fail = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    // Tensor memory is taken when the kernel in front has ended, and the one behind comes when this one has its own: none holds what another waits for.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (warp == kMma) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -226,7 +227,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
     fence_before();
     __syncthreads();
     fence_after();
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
     const uint32_t tmem = tmem_slot;
     const uint32_t tmem_s[2] = {tmem, tmem + 128}, tmem_o[2] = {tmem + 256, tmem + 256 + D};
     int32_t* status = a.c.status;
@@ -253,7 +254,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
             ++turn;
             return v;
         };
-        while (ok && line.next(a, g)) {
+        // A wait that gave up (recorded by mbar_wait, which then returns at once everywhere) does not end these loops: the two threads of a row meet at
+        // barriers that know no limit, so both go through all of them, whatever the numbers are.
+        while (line.next(a, g)) {
             if (tile == 1 && !two_tiles(g)) { blk += g.i1 - g.i0; continue; }
             const int col = g.ct * kRows + tile * 128 + row, qi = col / s.G;
             const bool there = qi < a.n_q;
@@ -401,8 +404,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                 }
             };
             for (int i = g.i0; i < g.i1; ++i, ++blk, ++n_s) {
-                ok = mbar_wait(bar.s_full + tile, n_s & 1, &fail, status);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                mbar_wait(bar.s_full + tile, n_s & 1, &fail, status);
+                __syncwarp();
                 fence_after();
                 const int marks = sc_marks[blk % kScSlots] >> (4 * half);           // (bits 0-3 and 8-11 are this half's)
                 if (i * kTok + 64 * half + 63 > sure || (marks & 0xf0f)) weights(std::true_type(), sc[blk % kScSlots] + 4 * half, marks, i);
@@ -412,8 +415,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar.p_full + tile);
             }
-            ok = ok && mbar_wait(bar.o_done + tile, n_o & 1, &fail, status);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            mbar_wait(bar.o_done + tile, n_o & 1, &fail, status);
+            __syncwarp();
             ++n_o;
             fence_after();
             float l0, l1;

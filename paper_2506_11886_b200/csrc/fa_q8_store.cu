@@ -286,7 +286,8 @@ template <typename T, int FMT>
 cudaError_t store_of(const Q8Dims& s, const Q8Cache& c, const void* K, const void* V, int64_t sb, int64_t st, int64_t sh, int n, const int32_t* n_row,
                      bool append, cudaStream_t stream) {
     // blocks that n tokens can touch behind a tail of blk - 1
-    const int64_t touched = n == 0 ? 1 : ((int64_t)(append ? s.blk - 1 : 0) + n - 1) / s.blk + 1;
+    int64_t touched = n == 0 ? 1 : ((int64_t)(append ? s.blk - 1 : 0) + n - 1) / s.blk + 1;
+    if (touched > s.nb + 1) touched = s.nb + 1;           // (rows that would need more are refused)
     const StoreArgs<T> a = {s, c, static_cast<const T*>(K), static_cast<const T*>(V), sb, st, sh, n, n_row, append, 1, s.d == 64 ? 6 : s.d == 128 ? 7 : 8};
     // 32 values to a thread, so that a block of the smallest size is a warp's; 64 or 128 where it is more than 256 threads'
     const int values = s.blk * s.d;

@@ -205,7 +205,7 @@ def test_rows_that_do_not_fit_and_pages_that_are_not_there():
 # ---- reading ----------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("d,block,t0,n", [(64, 16, 0, 100), (128, 64, 37, 150), (256, 32, 95, 1), (128, 128, 130, 60)])
+@pytest.mark.parametrize("d,block,t0,n", [(64, 16, 0, 100), (128, 64, 37, 150), (256, 32, 95, 1), (128, 128, 130, 60), (64, 32, 150, 100)])
 def test_read_gives_what_the_cache_stands_for(fmt, dtype, d, block, t0, n):
     """A value is code * scale with one rounding, and one to the dtype: half a step of fp32 for the scale, the product, then
     half a step of the dtype.  Tokens that a row does not hold, and what lies around the output, stay as they were."""

@@ -80,6 +80,9 @@ def test_bad_arguments():
     assert lib.fa_q8_read(C.byref(lay), C.byref(ok), 16, 16, 0, 1024, 128, -1, 4, None) == bad
     assert lib.fa_q8_read(C.byref(lay), C.byref(ok), 16, 16, 0, 1024, 128, 0x7fffffff, 4, None) == bad
     assert lib.fa_q8_append(C.byref(lay), C.byref(ok), None, None, 0, 0, 0, 0, None, None) == fa.FA_OK          # no tokens: nothing to do
+    assert lib.fa_q8_read(C.byref(lay), C.byref(ok), 16, 16, 0, 1024, 128, 512 * 64, 4, None) == fa.FA_OK       # behind what a row can hold
+    wide = _layout(batch=65535, n_kv_heads=4096, n_q_heads=4096).c()                                            # more blocks than a launch counts
+    assert lib.fa_q8_write(C.byref(wide), C.byref(ok), 16, 16, 0, 1024, 128, 1 << 20, None, None) == fa.FA_ERR_UNSUPPORTED
     assert lib.fa_q8_read(C.byref(lay), C.byref(ok), None, None, 0, 0, 0, 5, 0, None) == fa.FA_OK
 
     def attend(q=16, sb=0, si=4096, sg=128, out=16, n_q=1, ws=16, size=1 << 30):
