@@ -75,7 +75,6 @@ __device__ __forceinline__ uint32_t half2_rest(float a, float b, uint32_t hi) {
 }
 __device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
 
-
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there = true) {      // zeros if not there
     asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -218,8 +217,15 @@ struct Columns {
     __device__ __forceinline__ void mma_o(int mt, const uint32_t (&w)[NT][2], const uint32_t (&wl)[NT][2], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            mma16816(o[nt][mt], a0, a1, a2, a3, w[nt][0], w[nt][1]);
-            if constexpr (kF32) mma16816(o[nt][mt], a0, a1, a2, a3, wl[nt][0], wl[nt][1]);
+            if constexpr (kF32) {    // (the MMA's own sums are cut off, not rounded: over many units that would add up)
+                float c[4] = {0.f, 0.f, 0.f, 0.f};
+                mma16816(c, a0, a1, a2, a3, wl[nt][0], wl[nt][1]);
+                mma16816(c, a0, a1, a2, a3, w[nt][0], w[nt][1]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[nt][mt][k] += c[k];
+            } else {
+                mma16816(o[nt][mt], a0, a1, a2, a3, w[nt][0], w[nt][1]);
+            }
         }
     }
 };

@@ -327,6 +327,37 @@ def test_long_rows_and_many_parts(fmt):
         attend_and_check(lay, cache, rows, rand((B, 1, Hq, d), "bf16", 3), "bf16")
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_fp32_sums_over_long_rows_are_rounded_not_cut_off(fmt):
+    """q = 0, so every weight is 1 and a column's output the mean of its V, all of one sign: errors of one direction add up.
+    A warp sums about 700 units of 16 tokens.  Counted: weights in two halves 2^-22, the sums inside the MMAs of a unit 4 x 2^-23,
+    the join and the division 25 x 2^-24, and 700 additions rounded by at most 2^-24 of a sum that grows to the last one's
+    size, of either sign: a deviation of sqrt(700 / 3) / sqrt(3) x 2^-24 and six of those.  (Cut off instead: 700 x 2^-24.)"""
+    B, H, d, block, nb = 40, 4, 64, 128, 640
+    n = nb * block
+    one, src = make(B=1, Hq=H, H=H, d=d, block=block, nb=nb, fmt=fmt, dtype="f32")
+    V = rand((1, n, H, d), "f32", 1).abs() + 0.25
+    fa.fa_q8_write(one, src, V.flip(1), V)
+    lay = fa.Q8Layout(batch=B, n_q_heads=H, n_kv_heads=H, head_dim=d, block=block, max_blocks=nb, n_pages=one.n_pages, format=FMT[fmt],
+                      kv_dtype=fa.FA_F32, softmax_scale=0.125)
+    cache = fa.Q8Cache(lay)
+    for name in ("k_pages", "v_pages", "k_scale", "v_scale"):
+        getattr(cache, name).copy_(getattr(src, name))
+    cache.block_table.copy_(src.block_table.expand(B, nb))
+    cache.state[:, 0] = n
+    q = torch.zeros((B, 1, H, d), device="cuda")
+    out = torch.full_like(q, math.nan)
+    fa.fa_q8_attention(lay, cache, q, out, fa.new_q8_workspace(lay))
+    assert fa.fa_q8_poll_status(cache) == fa.FA_OK
+    page = src.block_table[0].long()
+    want = torch.zeros((H, d), dtype=torch.float64, device="cuda")
+    for i in range(nb):
+        want += src.v_pages[page[i]].double().sum(1) * src.v_scale[page[i]].double()[:, None]
+    want /= n
+    err = ((out.double().reshape(B, H, d) - want) / want).abs().max()
+    assert float(err) <= 2.0 ** -22 + 4 * 2.0 ** -23 + 25 * 2.0 ** -24 + 6 * math.sqrt(700 / 9) * 2.0 ** -24
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_blocks_of_very_different_scale(dtype):
     """V blocks (and a tail) from 1e-30 to 1e30, K blocks from 1e-6 on: a weight's share in the result goes by p times its block's scale."""
