@@ -16,7 +16,7 @@
 // joins them, spread over all SMs.
 // The loops of the roles share the instruction cache: what is unrolled (a row of scores in registers) is written once, the rest kept small.
 // The exponentials (16 a clock and SM) take 2048 clocks for a block and 256 rows of any head dim, the tensor cores as many at 128 dims; it is bound by the chain of a tile
-// (scores, maximum, exponentials, products), 5300 clocks, of which two run at a time: 2048 queries of 32/8 heads of 128 over 16384 tokens 650 us (793 TFLOP/s).
+// (scores, maximum, exponentials, products), 5300 clocks, of which two run at a time: 2048 queries of 32/8 heads of 128 over 16384 tokens 645 us (799 TFLOP/s), back to back 655.
 #include <type_traits>
 
 #include "fa_q8.cuh"
@@ -30,6 +30,10 @@ using namespace umma;
 constexpr int kRows = 256, kTok = 128;
 constexpr int kConv = 16, kMma = 20, kConvWarps = 7;       // first converting warp, the issuing warp, converting warps (16-19, 21-23)
 constexpr int kChunkThreads = 24 * 32;
+// Blocks whose outputs one accumulator takes, a power of two.  The MMAs' sums are cut off, not rounded: over 8192 blocks of V of one sign the outputs
+// came out 4.2e-3 of themselves too small.  After a run its sums go to the workspace, where they are added with rounding: 4e-4, which is no more
+// than the halves and the output lose.  Tiles below 32768 tokens to a CTA are one run; they pay 1 % for the branch (639 -> 645 us).
+constexpr int kRun = 256;
 constexpr int kScSlots = 4;                                // scales of blocks: a slot is free when the weights of the block two in front are done
 
 struct ChunkArgs {
@@ -403,10 +407,39 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                     tmem_st16(ts + 16 * c, w);
                 }
             };
+            // Parts of a tile lie one behind the other from 2 x its first CTA + 1 on (as in fa_q8_attn.cu); a tile that is not cut has a place there too.
+            // (Found anew where it is needed: registers are short in between.)
+            auto place = [&] {
+                unsigned cta;
+                asm volatile("mov.u32 %0, %%ctaid.x;" : "=r"(cta));
+                return a.part + ((size_t)(g.u / line.per + 1 + cta) * kRows + tile * 128 + row) * (D + 4);
+            };
             for (int i = g.i0; i < g.i1; ++i, ++blk, ++n_s) {
                 mbar_wait(bar.s_full + tile, n_s & 1, &fail, status);
                 __syncwarp();
                 fence_after();
+                if (i > g.i0 && ((i - g.i0) & (kRun - 1)) == 0) {      // (the MMAs of the block before are done, those of this one start from zero)
+                    float* part = place();
+                    const bool more = i - g.i0 > kRun;
+                    const float r = more ? pow2_down(part[D + half], mp) : 0.f;            // (the m' of what stands there)
+                    __syncwarp();
+#pragma unroll 1
+                    for (int c = 0; c < D / 2; c += 16) {
+                        uint32_t x[16];
+                        tmem_ld16(to + c, x);
+                        const int at = ((D / 2) * half + c) >> 3;
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4) {
+                            float4* p = reinterpret_cast<float4*>(part + dim_of<D>(at + (j >> 3)) + (j & 4));
+                            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (more) y = *p;
+                            *p = make_float4(fmaf(y.x, r, __uint_as_float(x[j])), fmaf(y.y, r, __uint_as_float(x[j + 1])),
+                                             fmaf(y.z, r, __uint_as_float(x[j + 2])), fmaf(y.w, r, __uint_as_float(x[j + 3])));
+                        }
+                        __syncwarp();
+                    }
+                    part[D + half] = mp;
+                }
                 const int marks = sc_marks[blk % kScSlots] >> (4 * half);           // (bits 0-3 and 8-11 are this half's)
                 if (i * kTok + 64 * half + 63 > sure || (marks & 0xf0f)) weights(std::true_type(), sc[blk % kScSlots] + 4 * half, marks, i);
                 else weights(std::false_type(), sc[blk % kScSlots] + 4 * half, marks, i);
@@ -422,14 +455,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
             float l0, l1;
             unpack2(l, l0, l1);
             l0 += l1;
+            float* part = place();
+            const bool runs = g.i1 - g.i0 > kRun;          // sums of the runs before stand in `part`
+            const float rh = runs ? pow2_down(part[D + half], mp) : 0.f;           // (read in front of the turn: the other thread writes here at the end)
             l1 = tell(make_float2(l0, 0.f)).x;
             l0 = half ? l1 + l0 : l0 + l1;
             const int e = (int)fminf(fmaxf(mp - m - 7.f, -250.f), 250.f);
             const float f1 = pow2i(e / 2), f2 = pow2i(e - e / 2), r = l0 == 0.f ? 0.f : 1.f / l0;
             const bool lone = g.i0 == 0 && g.i1 == g.n;
             __nv_bfloat16* o = a.out + (((size_t)g.b * a.n_q + qi) * s.Hq + g.h * s.G + col % s.G) * D;
-            // parts of a tile lie one behind the other from 2 x its first CTA + 1 on (as in fa_q8_attn.cu)
-            float* part = a.part + ((size_t)(g.u / line.per + 1 + blockIdx.x) * kRows + tile * 128 + row) * (D + 4);
 #pragma unroll 1
             for (int c = 0; c < D / 2; c += 16) {
                 uint32_t x[16];
@@ -441,6 +475,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
 #pragma unroll
                     for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(x[8 * j + k]);
                     const int dim = dim_of<D>(at + j);
+                    if (runs) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) y[k] = fmaf(part[dim + k], rh, y[k]);
+                    }
                     if (lone && there) {
                         uint32_t w[4];
 #pragma unroll
@@ -639,7 +677,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                         if (lane == 0) {
                             const uint32_t p = tmem + 128 * t, o = tmem + 256 + D * t;
 #pragma unroll
-                            for (int k = 0; k < kTok / 16; ++k) umma_ts(o, p + 8 * k + 32 * (k >> 2), vd + (uint64_t)(k * 2048 >> 4), kIdescO, i > 1 || k > 0);
+                            for (int k = 0; k < kTok / 16; ++k) umma_ts(o, p + 8 * k + 32 * (k >> 2), vd + (uint64_t)(k * 2048 >> 4), kIdescO, ((i - 1) & (kRun - 1)) != 0 || k > 0);
                             if (i == n) umma_commit(bar.o_done + t);
                         }
                         __syncwarp();

@@ -358,6 +358,70 @@ def test_fp32_sums_over_long_rows_are_rounded_not_cut_off(fmt):
     assert float(err) <= 2.0 ** -22 + 4 * 2.0 ** -23 + 25 * 2.0 ** -24 + 6 * math.sqrt(700 / 9) * 2.0 ** -24
 
 
+@pytest.mark.parametrize("fmt,d", [("int8", 128), ("e4m3", 64)])
+def test_a_chunk_at_the_end_of_a_million_tokens(fmt, d):
+    """q = 0: a column's output is the mean of its V, all of one sign.  A tile is summed by one or two CTAs over 8192 blocks of 128 tokens.
+    Counted: the output's half step, the weights' (halves, 2^-11), cut-offs of 2^-13 in runs of 256 blocks and 2^-13 for all that is rounded to 2^-24."""
+    B, H, G, block, held, nb, n_q = 2, 2, 8, 128, 512, 8192, 1024
+    n = nb * block
+    one, src = make(B=1, Hq=H, H=H, d=d, block=block, nb=held, fmt=fmt, extra=0)
+    V = (rand((1, held * block, H, d), "f32", 1, 0.0).abs() + 0.25).bfloat16()
+    fa.fa_q8_write(one, src, V, V)
+    lay = fa.Q8Layout(batch=B, n_q_heads=G * H, n_kv_heads=H, head_dim=d, block=block, max_blocks=nb, n_pages=held, format=FMT[fmt],
+                      kv_dtype=fa.FA_BF16, softmax_scale=0.125)
+    cache = fa.Q8Cache(lay)
+    for name in ("k_pages", "v_pages", "k_scale", "v_scale"):
+        getattr(cache, name).copy_(getattr(src, name))
+    table = torch.randint(0, held, (nb,), generator=torch.Generator().manual_seed(1))
+    cache.block_table.copy_(table.to(torch.int32).expand(B, nb))
+    cache.state[:, 0] = n
+    q = torch.zeros((B, n_q, G * H, d), dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, math.nan)
+    fa.fa_q8_attention(lay, cache, q, out, fa.new_q8_workspace(lay, n_q))
+    assert fa.fa_q8_poll_status(cache) == fa.FA_OK
+    block_sums = src.v_pages.double().sum(2) * src.v_scale.double()[:, :, None]
+    # all queries see the blocks in front of the last eight; the last one all of them
+    want = (block_sums * torch.bincount(table, minlength=held).double().cuda()[:, None, None]).sum(0) / n
+    err = ((out[:, -1].double().reshape(B, H, G, d) - want[None, :, None]) / want[None, :, None]).abs().max()
+    assert float(err) <= 2.0 ** -8 + 2.0 ** -11 + 2.0 ** -13 + 2.0 ** -13
+    # ... the first one the tokens up to its own
+    seen = n - n_q + 1
+    want = ((want * n) - sum(block_sums[table[i]] for i in range(nb - 8, nb)) + src.v_pages[table[nb - 8], :, 0].double() * src.v_scale[table[nb - 8]].double()[:, None]) / seen
+    err = ((out[:, 0].double().reshape(B, H, G, d) - want[None, :, None]) / want[None, :, None]).abs().max()
+    assert float(err) <= 2.0 ** -8 + 2.0 ** -11 + 2.0 ** -13 + 2.0 ** -13
+
+
+@pytest.mark.parametrize("scores", [3.0, 40.0])
+def test_runs_of_blocks_with_maxima_that_grow(scores):
+    """The sums of 256 blocks are put away while the maxima of the scores and of the values still grow, in tiles of one CTA and in cut ones."""
+    B, Hq, H, d, block, n, n_q = 170, 8, 1, 64, 64, 80000, 9
+    one, src = make(Hq=Hq, H=H, d=d, block=block, nb=1250, scale=1.0)
+    K, V = rand((1, n, H, d), "bf16", 1, 0.0), rand((1, n, H, d), "bf16", 2, 0.0)
+    ramp = torch.linspace(0.05, 1.0, n, device="cuda")[None, :, None, None]
+    K = (K.float() * ramp * scores / 24).bfloat16()
+    V = (V.float() * 2.0 ** (torch.arange(n, device="cuda") // 9000 - 4)[None, :, None, None]).bfloat16()
+    fa.fa_q8_write(one, src, K, V)
+    lay = fa.Q8Layout(batch=B, n_q_heads=Hq, n_kv_heads=H, head_dim=d, block=block, max_blocks=1250, n_pages=one.n_pages, format=fa.FA_Q8_INT8,
+                      kv_dtype=fa.FA_BF16, softmax_scale=1.0)
+    cache = fa.Q8Cache(lay)
+    for name in ("k_pages", "v_pages", "k_scale", "v_scale"):
+        getattr(cache, name).copy_(getattr(src, name))
+    cache.block_table.copy_(src.block_table.expand(B, 1250))
+    cache.state[:, 0] = n
+    rows = ref.Rows(1, H, d, block, "int8", torch.bfloat16)
+    rows.push(0, K[0], V[0])
+    k, v = rows.held("k", 0, 0), rows.held("v", 0, 0)
+    q = rand((B, n_q, Hq, d), "bf16", 3, 0.0)
+    out = torch.full_like(q, math.nan)
+    fa.fa_q8_attention(lay, cache, q, out, fa.new_q8_workspace(lay, n_q))
+    assert fa.fa_q8_poll_status(cache) == fa.FA_OK
+    assert torch.isfinite(out.float()).all()
+    for b in (0, 1, 60, 85, 118, 168, 169):
+        want, tol = ref.attention(k, v, q[b].cpu().double(), n_q, 1.0, torch.bfloat16)
+        err = (out[b].cpu().double() - want).abs()
+        assert (err <= tol).all(), (b, float((err / tol).max()))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_blocks_of_very_different_scale(dtype):
     """V blocks (and a tail) from 1e-30 to 1e30, K blocks from 1e-6 on: a weight's share in the result goes by p times its block's scale."""
