@@ -11,7 +11,8 @@
 // Scales: a score is multiplied by its block's K scale.  The weight of a token in O is w = p sv 2^(m - m' + 15), sv its block's
 // V scale, m the column's running maximum of the scores, m' that of score + exponent of sv, both rounded up to whole numbers (of log2), so
 // that rescaling is exact: w is at most 2^15 and its rounding to a half is relative to 2^-24 of the largest weight
-// or better; the sum of the p runs beside it in fp32.  The tail is the same with the power of two above its largest magnitude
+// or better; the sum of the p runs beside it in fp32.  The exponent of sv counts as -111 at least, which keeps 2^(m - m' + 15) a number: where all of V is
+// smaller, the weights are p sv 2^126 and use less of the range.  The tail is the same with the power of two above its largest magnitude
 // in the place of the scale.
 //
 // Work: a (row, head, column tile) pair has one unit for every 16 tokens in pages and one for the tail.  As long as there are fewer pairs than CTAs,
@@ -29,6 +30,8 @@ namespace {
 constexpr int kUnit = 16;            // tokens
 constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kFlat = 40;            // parts that one CTA joins in one go
+constexpr float kMinExp = -111.f;    // V scales count as 2^-112 at least in m'
+constexpr int kTailExp = -113;       // a tail's largest magnitude as this power of two at least: 2^(13 - kTailExp) is a number
 
 struct AttnArgs {
     Q8Dims s;
@@ -153,15 +156,17 @@ struct Columns {
             if constexpr (kF32) mma16816(s[nt], a0, a1, a2, a3, ql[nt][kt][0], ql[nt][kt][1]);
         }
     }
-    // The factor between p and the weights of V of scale 1.  m' <= m + 128 and m' >= m - 126: only the upper end can leave the range, for V scales
-    // below 2^-111, where the weights then use less of it.
+    // The factor between p and the weights of V of scale 1.  m' <= m + 128 and m' >= m - 111 (kMinExp): the exponent is in range (the bounds are for maxima
+    // of 2^24 and more, where m + exponent of sv is rounded).
     __device__ __forceinline__ void factor(int nt, int k) { g[nt][k] = pow2i((int)fminf(fmaxf(m[nt][k] - mp[nt][k] + 15.f, -126.f), 126.f)); }
     // Scores of a unit (as products) to weights; tok: the token of row g (masks only if `edge`).
     // low: products of q8 + 128 in the last bits.
     template <bool LOW>
     __device__ __forceinline__ void weights(float (&s)[NT][4], float ks, float vs, int tok, bool edge, uint32_t (&w)[NT][2], uint32_t (&wl)[NT][2]) {
-        const float ev = (float)(exponent_of(vs) + 1);
+        const float ev = fmaxf((float)(exponent_of(vs) + 1), kMinExp);
         ks = fmaf(vs, 0.f, ks);      // (a V scale that is NaN makes the scores so)
+        const float vf = fminf(vs, 0x1.fffffep127f);       // (finite: what is not seen is 0 x vf)
+        const Q8Two<float> v2 = Q8Two<float>::of(vf, vf);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const float f0 = f[nt][0] * ks, f1 = f[nt][1] * ks;
@@ -202,9 +207,11 @@ struct Columns {
             const float p0 = ex2(x[0] - m[nt][0]), p1 = ex2(x[1] - m[nt][1]), p2 = ex2(x[2] - m[nt][0]), p3 = ex2(x[3] - m[nt][1]);
             l[nt][0] += p0 + p2;
             l[nt][1] += p1 + p3;
-            // (a block whose scores are far below m may have a scale beyond the range: its p are zero then)
-            const float c0 = fminf(vs * g[nt][0], 0x1p127f), c1 = fminf(vs * g[nt][1], 0x1p127f);
-            const float w0 = p0 * c0, w1 = p1 * c1, w2 = p2 * c0, w3 = p3 * c1;
+            // w = p g sv, in this order: sv may be as many powers of two above the others as p is below one, and g sv beyond the range
+            const Q8Two<float> g2 = Q8Two<float>::of(g[nt][0], g[nt][1]);
+            float w0, w1, w2, w3;
+            Q8Two<float>::of(p0, p1).times(g2).times(v2).get(w0, w1);
+            Q8Two<float>::of(p2, p3).times(g2).times(v2).get(w2, w3);
             const uint32_t u0 = half2_of(w0, w1), u1 = half2_of(w2, w3);
             w[nt][0] = movmatrix_t(u0);
             w[nt][1] = movmatrix_t(u1);
@@ -317,7 +324,7 @@ __device__ __forceinline__ void unit_of_tail(Columns<T, D, NT>& C, const Tail<T>
     const int g = lane >> 2, t = lane & 3, row0 = sub * kUnit;
     // the power of two that brings the largest magnitude to 2^13 .. 2^14, where halves hold the values next to it in full
     const bool kbad = tl.kmax >= 0x7f800000u, vbad = tl.vmax >= 0x7f800000u;
-    const int ek = max((int)(tl.kmax >> 23) - 127, -100), evt = max((int)(tl.vmax >> 23) - 127, -100);
+    const int ek = max((int)(tl.kmax >> 23) - 127, kTailExp), evt = max((int)(tl.vmax >> 23) - 127, kTailExp);
     const float kf = pow2i(13 - ek), vf = pow2i(13 - evt);
     const float ks = kbad ? __uint_as_float(0x7fc00000u) : pow2i(ek - 13), vs = vbad ? __uint_as_float(0x7fc00000u) : pow2i(evt - 13);
     auto get = [&](Vec16<T>& x, int side, int r, int e) {            // 16 elements of row r of the unit; zeros behind the row's last token
