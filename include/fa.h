@@ -401,7 +401,10 @@ fa_status fa_q8_read(const fa_q8_layout* layout, const fa_q8_cache* cache, void*
  * g*stride_g + e (strides in elements, multiples of 8); out: [B][n_q][H_q][d].  The queries are those of the row's
  * last n_q tokens, whose K and V the cache holds already: query i sees tokens 0 .. len - n_q + i.  A query that sees none (an empty
  * row, or a row of fewer than n_q tokens) gives zeros.  out must not overlap q.  Does not modify the cache.  Tokens whose page is out of range are
- * left out and FA_ERR_INDEX is reported. */
+ * left out and FA_ERR_INDEX is reported.
+ * The work is counted in 32 bits, by what a row can hold.  With G = H_q / H_kv and N = max_blocks * block, FA_ERR_UNSUPPORTED beyond
+ * B * H_kv * ceil(n_q G / 256) * N / 128 = 2^31 - 1 for bf16 with d = 64 or 128 and more than 64 columns n_q G; otherwise beyond
+ * B * H_kv * ceil(n_q G / 16) * N / 16 = 2^31 - 1 (a little less: a tail counts too; up to 8 columns are one tile); and beyond n_q H_q = 2^26. */
 fa_status fa_q8_attention(const fa_q8_layout* layout, const fa_q8_cache* cache, const void* q, int64_t stride_b, int64_t stride_i,
                           int64_t stride_g, void* out, int32_t n_q, void* ws, size_t ws_bytes, void* stream);
 

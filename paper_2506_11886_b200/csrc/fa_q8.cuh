@@ -46,10 +46,10 @@ cudaError_t launch_q8_read(const Q8Dims&, const Q8Cache&, int fmt, int dtype, vo
                            cudaStream_t);
 // k_new / v_new non-null: a step (n_q = 1).
 size_t q8_attention_ws_bytes(const Q8Dims&, int n_q);
-bool q8_attention_fits(const Q8Dims&, int n_q);      // the units of work are counted in 32 bits
+bool q8_attention_fits(const Q8Dims&, int n_q);      // the units of work are counted in 32 bits (of calls that q8_chunk_takes does not take)
 cudaError_t launch_q8_attention(const Q8Dims&, const Q8Cache&, int fmt, int dtype, const void* q, int64_t sb, int64_t si, int64_t sg, void* out, int n_q,
                                 const void* k_new, const void* v_new, char* ws, cudaStream_t);
-// The same for many query columns to a KV head (fa_q8_chunk.cu).
+// The same for many query columns to a KV head, as far as their blocks are counted in 32 bits (fa_q8_chunk.cu).
 bool q8_chunk_takes(const Q8Dims&, int dtype, int n_q);
 size_t q8_chunk_ws_bytes(const Q8Dims&);
 cudaError_t launch_q8_chunk(const Q8Dims&, const Q8Cache&, int fmt, const void* q, int64_t sb, int64_t si, int64_t sg, void* out, int n_q, char* ws,

@@ -60,7 +60,7 @@ fa_status attention_call(const fa_q8_layout* layout, const fa_q8_cache* cache, c
     if (!q || !out || !aligned16(q) || !aligned16(out)) return FA_ERR_INVALID_ARG;
     if (sb < 0 || si < layout->head_dim || sg < layout->head_dim || ((sb | si | sg) & 7)) return FA_ERR_INVALID_ARG;
     const Q8Dims s = make_q8_dims(*layout);
-    if (!q8_attention_fits(s, n_q)) return FA_ERR_UNSUPPORTED;
+    if (!(k_new == nullptr && q8_chunk_takes(s, layout->kv_dtype, n_q)) && !q8_attention_fits(s, n_q)) return FA_ERR_UNSUPPORTED;
     if (!ws || !aligned16(ws) || ws_bytes < q8_attention_ws_bytes(s, n_q)) return FA_ERR_WORKSPACE;
     return launch_q8_attention(s, make_q8_cache(*cache), layout->format, layout->kv_dtype, q, sb, si, sg, out, n_q, k_new, v_new, static_cast<char*>(ws),
                                static_cast<cudaStream_t>(stream)) == cudaSuccess ? FA_OK : FA_ERR_CUDA;
