@@ -336,7 +336,9 @@ int fa_launch_count(const fa_layout* layout, int what);
  * rounded to 32 bits (down where top * scale would overflow).  A block of zeros has scale 0; a block with a value that is not finite has scale NaN and reads
  * as NaN throughout (attention treats a tail that holds one the same way).
  * Pages are found by a block table, so rows may share pages that they only read (a common prompt), and pages need no order.
- * A block needs its page when it becomes complete; entries of later blocks are not read. */
+ * A block needs its page when it becomes complete; entries of later blocks are not read.
+ * A row whose state is no length (below 0, above max_blocks * block) holds nothing for every call but fa_q8_write and fa_q8_reset, takes no tokens, and
+ * FA_ERR_CAPACITY is reported. */
 typedef enum { FA_Q8_INT8 = 0, FA_Q8_E4M3 = 1 } fa_q8_format;
 
 typedef struct fa_q8_layout {

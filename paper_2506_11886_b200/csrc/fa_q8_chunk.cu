@@ -62,10 +62,11 @@ __device__ __forceinline__ uint32_t half2_of(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Tokens of row b that the cache holds; those that column tile ct sees, in blocks of 128.
+__device__ __forceinline__ bool is_length(const ChunkArgs& a, int len) { return len >= 0 && len <= (a.s.nb << a.s.lb); }
+// Tokens of row b that the cache holds (none if its state is no length: the joining kernel reports that); those that column tile ct sees, in blocks of 128.
 __device__ __forceinline__ int row_len(const ChunkArgs& a, int b) {
     const int len = a.c.state[b * kQ8State];
-    return len < 0 || len > (a.s.nb << a.s.lb) ? 0 : len;
+    return is_length(a, len) ? len : 0;
 }
 __device__ __forceinline__ int blocks_of(const ChunkArgs& a, int len, int ct) {
     const int last = min(a.n_q - 1, (ct * kRows + kRows - 1) / a.s.G);
@@ -713,7 +714,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
     }
 }
 
-// Joins the parts of tiles that were cut, in the order of the tokens; zeros for tiles that see nothing.  A warp takes a row.
+// Joins the parts of tiles that were cut, in the order of the tokens; zeros for tiles that see nothing; rows whose state is no length are reported.  A warp
+// takes a row.
 template <int D>
 __global__ void __launch_bounds__(256) q8_chunk_join_kernel(const ChunkArgs a) {
     const Q8Dims& s = a.s;
@@ -722,6 +724,7 @@ __global__ void __launch_bounds__(256) q8_chunk_join_kernel(const ChunkArgs a) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int k = (int)(blockIdx.x / (unsigned)s.H), h = (int)(blockIdx.x % (unsigned)s.H);
     const int b = k / a.n_ct, ct = k % a.n_ct;
+    if (ct == 0 && h == 0 && blockIdx.y == 0 && threadIdx.x == 0 && !is_length(a, a.c.state[b * kQ8State])) q8_report(a.c.status, FA_ERR_CAPACITY);
     const int n = blocks_of(a, row_len(a, b), ct);
     Line line;
     unsigned u = 0, cta0 = 0, parts = 0;
