@@ -32,7 +32,8 @@ constexpr int kConv = 16, kMma = 20, kConvWarps = 7;       // first converting w
 constexpr int kChunkThreads = 24 * 32;
 // Blocks whose outputs one accumulator takes, a power of two.  The MMAs' sums are cut off, not rounded: over 8192 blocks of V of one sign the outputs
 // came out 4.2e-3 of themselves too small.  After a run its sums go to the workspace, where they are added with rounding: 4e-4, which is no more
-// than the halves and the output lose.  Tiles below 32768 tokens to a CTA are one run; they pay 1 % for the branch (639 -> 645 us).
+// than the halves and the output lose.  Tiles below 32768 tokens to a CTA are one run; they pay 1 % for the branch (639 -> 645 us).  The sums of p are kept in
+// the same runs: one sum over 2^24 tokens, rounded at every addition, was 0.8 % too small where all p were alike.
 constexpr int kRun = 256;
 constexpr int kScSlots = 4;                                // scales of blocks: a slot is free when the weights of the block two in front are done
 
@@ -165,11 +166,6 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
     f32x2 r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-    f32x2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -307,7 +303,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
             // the first token that some row of the warp does not see
             const int sure = __reduce_min_sync(0xffffffffu, there ? last : 0x7fffffff);
             float m = kNegBig, mp = kNegBig;
-            f32x2 l = pack2(0.f, 0.f);                     // of the even and the odd tokens of this half
+            float l = 0.f, l_runs = 0.f;                   // of this half's tokens: of the present run, of those before
             // The weights of block i.  edge: some row of the warp does not see all of its tokens, or some of them are in the tail.
             auto weights = [&](auto edge_of, const float2* scale, int marks, int i) {
                 constexpr bool edge = decltype(edge_of)::value;
@@ -367,7 +363,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                 if (__any_sync(0xffffffffu, grow)) {
                     const float m2 = grow ? fmaxf(m, ceilf(bm)) : m, p2 = grow ? fmaxf(mp, ceilf(bp)) : mp;
                     const float rl = pow2_down(m, m2), r = pow2_down(mp, p2);
-                    l = mul2(l, pack2(rl, rl));
+                    l *= rl;
+                    l_runs *= rl;
                     m = m2;
                     mp = p2;
                     if (i > g.i0) {
@@ -403,7 +400,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                             sum = add2(sum, pack2(y0, y1));
                             w[8 * h2 + (j >> 1)] = half2_of(y0, y1);
                         }
-                        l = fma2(sum, pack2(back, back), l);
+                        float s0, s1;
+                        unpack2(sum, s0, s1);
+                        l = fmaf(s0 + s1, back, l);
                     }
                     tmem_st16(ts + 16 * c, w);
                 }
@@ -440,6 +439,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                         __syncwarp();
                     }
                     part[D + half] = mp;
+                    l_runs += l;
+                    l = 0.f;
                 }
                 const int marks = sc_marks[blk % kScSlots] >> (4 * half);           // (bits 0-3 and 8-11 are this half's)
                 if (i * kTok + 64 * half + 63 > sure || (marks & 0xf0f)) weights(std::true_type(), sc[blk % kScSlots] + 4 * half, marks, i);
@@ -453,16 +454,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
             __syncwarp();
             ++n_o;
             fence_after();
-            float l0, l1;
-            unpack2(l, l0, l1);
-            l0 += l1;
+            l += l_runs;
             float* part = place();
             const bool runs = g.i1 - g.i0 > kRun;          // sums of the runs before stand in `part`
             const float rh = runs ? pow2_down(part[D + half], mp) : 0.f;           // (read in front of the turn: the other thread writes here at the end)
-            l1 = tell(make_float2(l0, 0.f)).x;
-            l0 = half ? l1 + l0 : l0 + l1;
+            const float l_other = tell(make_float2(l, 0.f)).x;
+            l = half ? l_other + l : l + l_other;
             const int e = (int)fminf(fmaxf(mp - m - 7.f, -250.f), 250.f);
-            const float f1 = pow2i(e / 2), f2 = pow2i(e - e / 2), r = l0 == 0.f ? 0.f : 1.f / l0;
+            const float f1 = pow2i(e / 2), f2 = pow2i(e - e / 2), r = l == 0.f ? 0.f : 1.f / l;
             const bool lone = g.i0 == 0 && g.i1 == g.n;
             __nv_bfloat16* o = a.out + (((size_t)g.b * a.n_q + qi) * s.Hq + g.h * s.G + col % s.G) * D;
 #pragma unroll 1
@@ -496,7 +495,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) q8_chunk_kernel(const ChunkA
                 }
                 __syncwarp();
             }
-            if (!lone && half == 0) *reinterpret_cast<float4*>(part + D) = make_float4(m, mp, l0, 0.f);
+            if (!lone && half == 0) *reinterpret_cast<float4*>(part + D) = make_float4(m, mp, l, 0.f);
             fence_before();                                // the next segment's MMAs come behind its first p_full
         }
     } else if (warp != kMma) {
