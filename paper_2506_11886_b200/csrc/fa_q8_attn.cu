@@ -30,6 +30,11 @@ namespace {
 constexpr int kUnit = 16;            // tokens
 constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kFlat = 40;            // parts that one CTA joins in one go
+// Units whose sums a warp keeps in registers.  The MMAs' sums are cut off, not rounded, and rounded ones of equal addends err one way too: over 131072 units
+// outputs of one sign came out 1.2e-2 too small, fp32 ones 5e-5.  After a run the sums go to the workspace, where they are added with rounding.  Rows below
+// 131072 tokens to a CTA are one run; the branch costs up to 2 % (32001 tokens 22.7 -> 23.1 us).
+constexpr int kRun = 1024;
+__host__ __device__ constexpr int run_floats(int d, int nt) { return nt * (d / 4 + 6); }         // of a lane: outputs; m, m', sum of p of its two columns
 constexpr float kMinExp = -111.f;    // V scales count as 2^-112 at least in m'
 constexpr int kTailExp = -113;       // a tail's largest magnitude as this power of two at least: 2^(13 - kTailExp) is a number
 
@@ -44,6 +49,7 @@ struct AttnArgs {
     const void *k_new, *v_new;       // a step
     unsigned* tickets;
     float* part;                     // [2 * CTAs][cols][D + 4]
+    float* runs;                     // [CTAs][warps][run_floats][32]; none where no warp can have more than kRun units
 };
 
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -219,6 +225,28 @@ struct Columns {
                 wl[nt][0] = movmatrix_t(half2_rest(w0, w1, u0));
                 wl[nt][1] = movmatrix_t(half2_rest(w2, w3, u1));
             }
+        }
+    }
+    // Adds what the lane's places p, p + 32, ... hold of the runs before (if `more`); PUT: leaves the sums there and starts anew.
+    template <bool PUT>
+    __device__ __forceinline__ void join_runs(float* p, bool more) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float r[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k, p += 96) {
+                r[k] = more ? pow2_down(p[32], mp[nt][k]) : 0.f;
+                if (more) l[nt][k] = fmaf(p[64], pow2_down(p[0], m[nt][k]), l[nt][k]);
+                if constexpr (PUT) { p[0] = m[nt][k]; p[32] = mp[nt][k]; p[64] = l[nt][k]; l[nt][k] = 0.f; }
+            }
+#pragma unroll
+            for (int i = 0; i < kMt; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k, p += 32) {
+                    float& x = o[nt][i][k];
+                    if (more) x = fmaf(p[0], r[k & 1], x);
+                    if constexpr (PUT) { p[0] = x; x = 0.f; }
+                }
         }
     }
     __device__ __forceinline__ void mma_o(int mt, const uint32_t (&w)[NT][2], const uint32_t (&wl)[NT][2], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
@@ -764,8 +792,11 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
 #pragma unroll
         for (int i = 1; i < kAhead; ++i) issue((R::kFirst + i) % R::kStages, u + i * kWarps, pages[i]);
         int stage = R::kFirst, page1 = page_of(u + kAhead * kWarps);
+        const int u_first = u;
+        auto runs = [&] { return a.runs + ((size_t)blockIdx.x * kWarps + warp) * (run_floats(D, NT) * 32) + lane; };
 #pragma unroll 1
         for (; u < stop; u += kWarps) {
+            if (u != u_first && ((u - u_first) & (kRun * kWarps - 1)) == 0) C.template join_runs<true>(runs(), u - u_first > kRun * kWarps);
             cp_wait<kAhead - 1>();
             __syncwarp();
             const int page2 = page_of(u + (kAhead + 1) * kWarps);
@@ -779,6 +810,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
             if (++stage == R::kStages) stage = 0;
             __syncwarp();
         }
+        if (u - u_first > kRun * kWarps) C.template join_runs<false>(runs(), true);
         cp_wait<0>();
         __syncthreads();                                   // the rings give way to the sums
         // ---- join the warps ----
@@ -882,7 +914,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
 struct Q8Plan {
     int nt, n_ct, ctas;
     long long units;                 // of all pairs, at most
-    size_t smem, part;
+    size_t smem, part, runs;
 };
 Q8Plan plan_q8(const Q8Dims& s, int n_q, int elt) {
     Q8Plan p;
@@ -901,6 +933,7 @@ Q8Plan plan_q8(const Q8Dims& s, int n_q, int elt) {
     p.smem = rings > sums ? rings : sums;
     if (heads > p.smem) p.smem = heads;
     p.part = (size_t)2 * p.ctas * per * (s.d + 4) * sizeof(float);
+    p.runs = (long long)s.nb * s.blk > (long long)kRun * kWarps * kUnit ? (size_t)p.ctas * kWarps * run_floats(s.d, p.nt) * 32 * sizeof(float) : 0;
     return p;
 }
 
@@ -923,7 +956,8 @@ cudaError_t attn_dims(const AttnArgs& a, const Q8Plan& p, cudaStream_t stream) {
 }  // namespace
 
 size_t q8_attention_ws_bytes(const Q8Dims& s, int n_q) {
-    const size_t a = 4096 + plan_q8(s, n_q, 2).part, b = 4096 + plan_q8(s, n_q, 4).part, c = q8_chunk_takes(s, FA_BF16, n_q) ? q8_chunk_ws_bytes(s) : 0;
+    const Q8Plan p = plan_q8(s, n_q, 2), p4 = plan_q8(s, n_q, 4);
+    const size_t a = 4096 + p.part + p.runs, b = 4096 + p4.part + p4.runs, c = q8_chunk_takes(s, FA_BF16, n_q) ? q8_chunk_ws_bytes(s) : 0;
     return a > b ? (a > c ? a : c) : (b > c ? b : c);
 }
 
@@ -933,7 +967,8 @@ cudaError_t launch_q8_attention(const Q8Dims& s, const Q8Cache& c, int fmt, int 
                                 const void* k_new, const void* v_new, char* ws, cudaStream_t stream) {
     if (!k_new && q8_chunk_takes(s, dtype, n_q)) return launch_q8_chunk(s, c, fmt, q, sb, si, sg, out, n_q, ws, stream);
     const Q8Plan p = plan_q8(s, n_q, dtype == FA_BF16 ? 2 : 4);
-    const AttnArgs a = {s, c, q, sb, si, sg, out, n_q, p.n_ct, (int)(p.ctas / ((long long)s.H * p.n_ct)), k_new, v_new, reinterpret_cast<unsigned*>(ws), reinterpret_cast<float*>(ws + 4096)};
+    const AttnArgs a = {s, c, q, sb, si, sg, out, n_q, p.n_ct, (int)(p.ctas / ((long long)s.H * p.n_ct)), k_new, v_new, reinterpret_cast<unsigned*>(ws), reinterpret_cast<float*>(ws + 4096),
+                        p.runs ? reinterpret_cast<float*>(ws + 4096 + p.part) : nullptr};
     if (dtype == FA_BF16) return fmt == FA_Q8_INT8 ? attn_dims<__nv_bfloat16, FA_Q8_INT8>(a, p, stream) : attn_dims<__nv_bfloat16, FA_Q8_E4M3>(a, p, stream);
     return fmt == FA_Q8_INT8 ? attn_dims<float, FA_Q8_INT8>(a, p, stream) : attn_dims<float, FA_Q8_E4M3>(a, p, stream);
 }

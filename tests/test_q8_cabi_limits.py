@@ -33,3 +33,11 @@ def test_chunks_over_long_block_tables():
     assert _call(2048, 1 << 40, batch=8192) == fa.FA_ERR_UNSUPPORTED
     # a few queries of the same rows
     assert _call(16, 4096) == fa.FA_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("tokens", [4096, 131072, 131072 + 128, 1 << 20, 1 << 24])
+@pytest.mark.parametrize("B,Hq,H,d", [(1, 32, 8, 128), (300, 1, 1, 64), (40, 80, 8, 256), (2, 8, 8, 64), (1, 4, 1, 256)])
+def test_a_workspace_serves_fewer_queries_too(tokens, B, Hq, H, d):
+    lay = fa.Q8Layout(batch=B, n_q_heads=Hq, n_kv_heads=H, head_dim=d, block=128, max_blocks=tokens // 128, n_pages=8)
+    sizes = [fa.fa_q8_workspace_bytes(lay, n) for n in (1, 2, 3, 5, 8, 9, 16, 17, 40, 64, 65, 300)]
+    assert sizes == sorted(sizes) and sizes[-1] < 256 << 20
