@@ -149,3 +149,38 @@ def test_chunks_of_blocks_of_very_different_scale():
         rows = ref.Rows(1, H, d, block, "int8", torch.bfloat16)
         rows.push(0, K[0], V[0])
         attend_and_check(lay, cache, rows, rand((1, n_q, Hq, d), "bf16", 3), "bf16")
+
+
+def test_captured_appends_chunks_and_reads():
+    """A graph of an append, the attention of the chunk and a read, replayed while the rows grow; bit for bit what the eager calls give."""
+    B, Hq, H, d, block, n = 2, 8, 2, 128, 16, 24
+    made = [make(B=B, Hq=Hq, H=H, d=d, block=block, nb=10) for _ in range(2)]
+    K, V, q = rand((B, n, H, d), "bf16", 1), rand((B, n, H, d), "bf16", 2), rand((B, n, Hq, d), "bf16", 3)
+    count = torch.tensor([n, n - 5], dtype=torch.int32, device="cuda")
+    outs = [[torch.zeros_like(q), torch.zeros((B, 160, H, d), dtype=q.dtype, device="cuda"), torch.zeros((B, 160, H, d), dtype=q.dtype, device="cuda")] for _ in range(2)]
+    ws = [fa.new_q8_workspace(made[0][0], n) for _ in range(2)]
+
+    def run(i, stream=None):
+        lay, cache = made[i]
+        fa.fa_q8_append(lay, cache, K, V, count, stream=stream)
+        fa.fa_q8_attention(lay, cache, q, outs[i][0], ws[i], stream=stream)
+        fa.fa_q8_read(lay, cache, outs[i][1], outs[i][2], stream=stream)
+
+    run(1)                                                             # (the first calls set the kernels' attributes)
+    fa.fa_q8_reset(*made[1])
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        run(0, side)
+    for i in range(7):                                                 # the last one is refused for row 0: 168 tokens
+        K.copy_(rand(K.shape, "bf16", 10 + i))
+        q.copy_(rand(q.shape, "bf16", 30 + i))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graph.replay()
+        torch.cuda.synchronize()
+        run(1)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(*outs)), i
+        assert made[0][1].state[:, 0].tolist() == made[1][1].state[:, 0].tolist() == [min(24 * (i + 1), 144), 19 * (i + 1)]
+    assert [fa.fa_q8_poll_status(c) for _, c in made] == [fa.FA_ERR_CAPACITY] * 2
