@@ -32,7 +32,7 @@ constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kFlat = 40;            // parts that one CTA joins in one go
 // Units whose sums a warp keeps in registers.  The MMAs' sums are cut off, not rounded, and rounded ones of equal addends err one way too: over 131072 units
 // outputs of one sign came out 1.2e-2 too small, fp32 ones 5e-5.  After a run the sums go to the workspace, where they are added with rounding.  Rows below
-// 131072 tokens to a CTA are one run; the branch costs up to 2 % (32001 tokens 22.7 -> 23.1 us).
+// 131072 tokens to a CTA are one run; they pay up to 2 % for the loop around (32001 tokens 22.7 -> 23.1 us).
 constexpr int kRun = 1024;
 __host__ __device__ constexpr int run_floats(int d, int nt) { return nt * (d / 4 + 6); }         // of a lane: outputs; m, m', sum of p of its two columns
 constexpr float kMinExp = -111.f;    // V scales count as 2^-112 at least in m'
@@ -172,7 +172,6 @@ struct Columns {
         const float ev = fmaxf((float)(exponent_of(vs) + 1), kMinExp);
         ks = fmaf(vs, 0.f, ks);      // (a V scale that is NaN makes the scores so)
         const float vf = fminf(vs, 0x1.fffffep127f);       // (finite: what is not seen is 0 x vf)
-        const Q8Two<float> v2 = Q8Two<float>::of(vf, vf);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const float f0 = f[nt][0] * ks, f1 = f[nt][1] * ks;
@@ -214,10 +213,14 @@ struct Columns {
             l[nt][0] += p0 + p2;
             l[nt][1] += p1 + p3;
             // w = p g sv, in this order: sv may be as many powers of two above the others as p is below one, and g sv beyond the range
-            const Q8Two<float> g2 = Q8Two<float>::of(g[nt][0], g[nt][1]);
             float w0, w1, w2, w3;
-            Q8Two<float>::of(p0, p1).times(g2).times(v2).get(w0, w1);
-            Q8Two<float>::of(p2, p3).times(g2).times(v2).get(w2, w3);
+            if constexpr (kF32) {
+                w0 = p0 * g[nt][0] * vf; w1 = p1 * g[nt][1] * vf; w2 = p2 * g[nt][0] * vf; w3 = p3 * g[nt][1] * vf;
+            } else {                 // (packed 2 % faster with many pairs; of fp32, 10 % slower)
+                const Q8Two<float> g2 = Q8Two<float>::of(g[nt][0], g[nt][1]), v2 = Q8Two<float>::of(vf, vf);
+                Q8Two<float>::of(p0, p1).times(g2).times(v2).get(w0, w1);
+                Q8Two<float>::of(p2, p3).times(g2).times(v2).get(w2, w3);
+            }
             const uint32_t u0 = half2_of(w0, w1), u1 = half2_of(w2, w3);
             w[nt][0] = movmatrix_t(u0);
             w[nt][1] = movmatrix_t(u1);
@@ -792,25 +795,31 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && D <= 128 && sizeof(T) == 
 #pragma unroll
         for (int i = 1; i < kAhead; ++i) issue((R::kFirst + i) % R::kStages, u + i * kWarps, pages[i]);
         int stage = R::kFirst, page1 = page_of(u + kAhead * kWarps);
-        const int u_first = u;
         auto runs = [&] { return a.runs + ((size_t)blockIdx.x * kWarps + warp) * (run_floats(D, NT) * 32) + lane; };
+        bool more = false;                                 // sums of runs are in the workspace
 #pragma unroll 1
-        for (; u < stop; u += kWarps) {
-            if (u != u_first && ((u - u_first) & (kRun * kWarps - 1)) == 0) C.template join_runs<true>(runs(), u - u_first > kRun * kWarps);
-            cp_wait<kAhead - 1>();
-            __syncwarp();
-            const int page2 = page_of(u + (kAhead + 1) * kWarps);
-            page1 = checked(u + kAhead * kWarps, page1);
-            issue(stage == 0 ? R::kStages - 1 : stage - 1, u + kAhead * kWarps, page1);          // (the stage read last)
-            if (pages[0] >= 0) unit_of_page<T, FMT, D, NT>(C, ring + (uint32_t)(stage * R::kBytes), u * kUnit + g, u * kUnit + kUnit > sure, lane);
+        for (int run_stop = min(stop, u + kRun * kWarps);;) {
+#pragma unroll 1
+            for (; u < run_stop; u += kWarps) {
+                cp_wait<kAhead - 1>();
+                __syncwarp();
+                const int page2 = page_of(u + (kAhead + 1) * kWarps);
+                page1 = checked(u + kAhead * kWarps, page1);
+                issue(stage == 0 ? R::kStages - 1 : stage - 1, u + kAhead * kWarps, page1);          // (the stage read last)
+                if (pages[0] >= 0) unit_of_page<T, FMT, D, NT>(C, ring + (uint32_t)(stage * R::kBytes), u * kUnit + g, u * kUnit + kUnit > sure, lane);
 #pragma unroll
-            for (int i = 0; i + 1 < kAhead; ++i) pages[i] = pages[i + 1];
-            pages[kAhead - 1] = page1;
-            page1 = page2;
-            if (++stage == R::kStages) stage = 0;
-            __syncwarp();
+                for (int i = 0; i + 1 < kAhead; ++i) pages[i] = pages[i + 1];
+                pages[kAhead - 1] = page1;
+                page1 = page2;
+                if (++stage == R::kStages) stage = 0;
+                __syncwarp();
+            }
+            if (u >= stop) break;
+            C.template join_runs<true>(runs(), more);
+            more = true;
+            run_stop = min(stop, u + kRun * kWarps);
         }
-        if (u - u_first > kRun * kWarps) C.template join_runs<false>(runs(), true);
+        if (more) C.template join_runs<false>(runs(), true);
         cp_wait<0>();
         __syncthreads();                                   // the rings give way to the sums
         // ---- join the warps ----
