@@ -336,6 +336,9 @@ int fa_launch_count(const fa_layout* layout, int what);
  * rounded to 32 bits (down where top * scale would overflow).  A block of zeros has scale 0; a block with a value that is not finite has scale NaN and reads
  * as NaN throughout (attention treats a tail that holds one the same way).
  * Pages are found by a block table, so rows may share pages that they only read (a common prompt), and pages need no order.
+ * Pages and scales may come from elsewhere: any byte with any finite scale, but no NaN code of e4m3 (0x7f, 0xff), which queries that do not see its
+ * token would meet too; NaN belongs into the scale.  A row's length may be set from outside to a multiple of `block`; other lengths only by the
+ * calls, which write the tail and tail_amax with them (so tokens cannot be taken back one by one).
  * A block needs its page when it becomes complete; entries of later blocks are not read.
  * A row whose state is no length (below 0, above max_blocks * block) holds nothing for every call but fa_q8_write and fa_q8_reset, takes no tokens, and
  * FA_ERR_CAPACITY is reported. */
@@ -404,6 +407,9 @@ fa_status fa_q8_read(const fa_q8_layout* layout, const fa_q8_cache* cache, void*
  * last n_q tokens, whose K and V the cache holds already: query i sees tokens 0 .. len - n_q + i.  A query that sees none (an empty
  * row, or a row of fewer than n_q tokens) gives zeros.  out must not overlap q.  Does not modify the cache.  Tokens whose page is out of range are
  * left out and FA_ERR_INDEX is reported.
+ * Logits, the softmax and the sums are held in 32 bits; for logits (times log2 e) up to 2^22, beyond which such numbers do not tell neighbours apart.  bf16:
+ * a weight times its block's V scale is rounded to 11 bits, so a result is off by 2^-11 of the mean of |V| beside its own rounding.  fp32: q, weights
+ * and tails are taken as two halves of 11 bits each, which leaves some 1e-6 of the mean of |V|.
  * The work is counted in 32 bits, by what a row can hold.  With G = H_q / H_kv and N = max_blocks * block, FA_ERR_UNSUPPORTED beyond
  * B * H_kv * ceil(n_q G / 256) * N / 128 = 2^31 - 1 for bf16 with d = 64 or 128 and more than 64 columns n_q G; otherwise beyond
  * B * H_kv * ceil(n_q G / 16) * N / 16 = 2^31 - 1 (a little less: a tail counts too; up to 8 columns are one tile); and beyond n_q H_q = 2^26. */

@@ -21,7 +21,7 @@
 // unit by itself, through a ring of its own in shared memory (cp.async, 16-byte chunks permuted so that the operand reads meet all banks);
 // the warps join in shared memory, the parts of a pair in the workspace, by the last CTA to finish, in the order of the tokens.
 // Bound by HBM for long rows, by the chain lengths - page - values - join for short ones.  32/8 heads of 128, one row of 128 / 1003 / 8192 / 32001 / 131000 tokens:
-// 5.2 / 8.4 / 12.4 / 21.1 / 53.6 us (int8), four rows of 131000 177 us (e4m3, 6.07 TB/s; back to back, at the clocks of the power cap, 187).
+// 6.4 / 9.5 / 12.2 / 23.1 / 56 us (int8), four rows of 131000 190 us (e4m3, 5.65 TB/s, back to back, at the clocks of the power cap); from one GPU to another up to 6 % apart.
 #include "fa_q8.cuh"
 
 namespace fa {

@@ -16,7 +16,8 @@
 // joins them, spread over all SMs.
 // The loops of the roles share the instruction cache: what is unrolled (a row of scores in registers) is written once, the rest kept small.
 // The exponentials (16 a clock and SM) take 2048 clocks for a block and 256 rows of any head dim, the tensor cores as many at 128 dims; it is bound by the chain of a tile
-// (scores, maximum, exponentials, products), 5300 clocks, of which two run at a time: 2048 queries of 32/8 heads of 128 over 16384 tokens 645 us (799 TFLOP/s), back to back 655.
+// (scores, maximum, exponentials, products), 5300 clocks, of which two run at a time: 2048 queries of 32/8 heads of 128 over 16384 tokens 650 us (793 TFLOP/s; e4m3
+// 669).  Registers are bounded at 80 a thread: 60 to 124 bytes are spilled.
 #include <type_traits>
 
 #include "fa_q8.cuh"
@@ -783,7 +784,8 @@ cudaError_t chunk_of(const ChunkArgs& a, cudaStream_t stream) {
 
 bool q8_chunk_takes(const Q8Dims& s, int dtype, int n_q) {
     // Over 64 columns to a KV head: one row of 16384 tokens, 32/8 heads of 128, us here / by tiles of 16 columns: 64 columns 55 / 49, 128 56 / 86,
-    // 256 68 / 155; of 1000 tokens 128 columns 24 / 17, 512 30 / 40; eight rows of 4000 tokens 64 columns 68 / 87.
+    // 256 68 / 155; of 1000 tokens 128 columns 24 / 17, 512 30 / 40; eight rows of 4000 tokens 64 columns 68 / 87.  The rows' lengths, by which this would
+    // go as well, are on the device: columns alone decide, which costs the short rows of these 7 us and the eight rows 19.
     if (dtype != FA_BF16 || s.d > 128 || (long long)n_q * s.G <= 64) return false;
     const long long tiles = (long long)s.B * chunk_tiles(s, n_q);
     return tiles * s.H * (((long long)s.nb * s.blk + kTok - 1) / kTok) <= 0x7fffffff && tiles * s.H <= 0x7fffffff;
